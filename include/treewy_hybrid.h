@@ -1,0 +1,137 @@
+/*
+ * treewy_hybrid.h - what a decode round of a gated-delta hybrid needs beside
+ * the gated-delta layers' calls of treewy.h, in the same library: the softmax
+ * layers' attention over a draft tree and a paged cache, that cache's commit,
+ * and the target's tokens drawn from its logits.
+ *
+ * A round: treewy_tree_attention reads the cached context and the draft's own
+ * keys and values (no rejected node ever reaches the cache), treewy_sample
+ * draws the target's token at every node, treewy_accept_greedy (treewy.h)
+ * keeps the path whose draft tokens equal them, and treewy_cache_append writes
+ * that path's keys and values into the cache, as treewy_commit does for a
+ * gated-delta state.  A prompt enters by chunks of up to 256 tokens: a chain
+ * (parent == NULL) attends, then treewy_cache_append without a path appends.
+ *
+ * The conventions of treewy.h hold (device pointers, caller-owned buffers,
+ * asynchronous on `stream`, the same status codes, flags OR-ed into err[b]),
+ * with two differences:
+ *  - q, k, v and o are [B, heads, N, d] by strides (treewy_strides): d is
+ *    contiguous, the other three are free, so that parts of one projection's
+ *    output need no copy.  A row's address is a multiple of 16 bytes: the base
+ *    is, and every stride of a dimension longer than one is too.
+ *  - treewy_tree_attention takes a workspace, whose size
+ *    treewy_tree_attention_workspace gives.  Its contents matter during the
+ *    call only, so that one buffer serves every call on a stream.
+ */
+#ifndef TREEWY_HYBRID_H
+#define TREEWY_HYBRID_H
+
+#include <stddef.h>
+
+#include "treewy.h"
+
+#ifdef __cplusplus
+extern "C" {
+#endif
+
+#define TREEWY_FLAG_BAD_PAGE 4    /* a page id outside [0, n_pages): its keys are left out, its tokens not written */
+#define TREEWY_FLAG_CACHE_FULL 8  /* cache_len negative or past the page table, or positions past the rotation table */
+#define TREEWY_FLAG_NO_TOKEN 16   /* a row of logits without a value above -inf (err[r] of treewy_sample) */
+
+/* Elements between two sequences, two heads, two tokens. */
+typedef struct treewy_strides {
+    int64_t seq, head, token;
+} treewy_strides;
+
+/* A cache of keys and values in pages of page_size tokens (a power of two, 8 to 4096).  Token p of sequence b is row
+ * p % page_size of page page_table[b][p / page_size]; entries past the sequence's tokens are not read. */
+typedef struct treewy_cache {
+    void *k, *v;                  /* [n_pages, H_kv, page_size, d] in the call's dtype, contiguous */
+    const int32_t *page_table;    /* [B, max_pages] */
+    const int32_t *len;           /* [B] tokens that the cache holds of each sequence */
+    int n_pages, max_pages, page_size;
+} treewy_cache;
+
+/* Rotation of the first `dims` values of a head (0: none; a multiple of 16, at most d): values i and i + dims/2 are a
+ * pair, turned by the angle whose cosine and sine cos[p][i] and sin[p][i] hold for position p. */
+typedef struct treewy_rotation {
+    const float *cos, *sin;       /* [positions, dims / 2] float32 */
+    int positions, dims;
+} treewy_rotation;
+
+/*
+ * treewy_cache_append - rotate keys to their positions and append keys and values to the paged cache.
+ *   k, v     [B, H_kv, N, d] dtype, by strides; keys not rotated yet
+ *   cache    pages are written; len is read
+ *   path     [B, L_max] int32 or NULL      nodes to append in order, as treewy_accept_greedy writes them; NULL: tokens
+ *                                          0, 1, ... themselves (then L_max = N)
+ *   count    [B] int32 or NULL             how many (path_len); NULL: all L_max
+ *   new_len  [B] int32 written             cache.len + count; not the buffer of cache.len
+ *   err      [B] int32 or NULL
+ * Entry l of sequence b goes to position cache.len[b] + l.  A sequence whose path is not strictly increasing within [0, N) or
+ * whose count is outside [0, L_max] (BAD_PATH), or which the page table or the rotation table has no room for (CACHE_FULL),
+ * appends nothing and keeps its length.  A token whose page id is invalid is not written (BAD_PAGE).
+ * d is 64, 128 or 256; N and L_max of a path are at most 256 (any N without one).  Each page belongs to one sequence here: two
+ * sequences that append to one page must not meet in a row.  One rounding: a rotated bf16 key, to nearest even.
+ */
+treewy_status treewy_cache_append(const void *k, treewy_strides k_strides, const void *v, treewy_strides v_strides,
+                                  const treewy_cache *cache, const treewy_rotation *rotation, const int32_t *path, int L_max,
+                                  const int32_t *count, int N, int B, int H_kv, int d, treewy_dtype dtype, int32_t *new_len,
+                                  int32_t *err, void *stream);
+
+/*
+ * treewy_tree_attention - softmax attention of every draft node over the cached context, its ancestors and itself:
+ *   o[b,h,t] = sum_j p_j v_j,  p = softmax_j(scale * (R q[b,h,t]) . k_j),
+ * over the cached keys j < len[b] of head h / (H_q / H_kv), and the draft's own keys of t's ancestors and of t, which are
+ * rotated as the cache will hold them.  Node t stands at position len[b] + (number of its ancestors).
+ *   q        [B, H_q, N, d] dtype, by strides, not rotated yet
+ *   k, v     [B, H_kv, N, d] dtype, by strides, not rotated yet
+ *   parent   [B, N] int32, or NULL: a chain (causal)
+ *   shared_len                             the first shared_len cached tokens (or as many as a sequence has) are the same for
+ *                                          every sequence, in the same pages: their keys are then read once for the whole
+ *                                          batch where that pays (few nodes).  0: nothing is known to be shared.  The result
+ *                                          is that of shared_len = 0 but for the order of sums.
+ *   o        [B, H_q, N, d] dtype, by strides, written
+ *   workspace                              at least treewy_tree_attention_workspace(...) bytes, 16-byte aligned
+ *   err      [B] int32 or NULL             BAD_PARENT (that parent counts as -1), BAD_PAGE, CACHE_FULL (a length outside
+ *                                          the table counts as the nearest inside; past the rotation table its last row)
+ * 1 <= N <= 256, d is 64, 128 or 256, H_q a multiple of H_kv.  Scores, softmax and sums are fp32; bf16 calls round the rotated
+ * q and k, the likelihoods that multiply v, and o.  Neither rows past len[b] in a page nor pages past it are used, whatever
+ * they hold.  Every call repeats itself bit for bit.
+ */
+treewy_status treewy_tree_attention(const void *q, treewy_strides q_strides, const void *k, treewy_strides k_strides,
+                                    const void *v, treewy_strides v_strides, const int32_t *parent, const treewy_cache *cache,
+                                    const treewy_rotation *rotation, int shared_len, float scale, int N, int B, int H_q,
+                                    int H_kv, int d, treewy_dtype dtype, void *o, treewy_strides o_strides, void *workspace,
+                                    size_t workspace_bytes, int32_t *err, void *stream);
+
+/* Bytes that treewy_tree_attention needs for calls of these sizes on the current device (0 for sizes that it refuses). */
+size_t treewy_tree_attention_workspace(int shared_len, int N, int B, int H_q, int H_kv, int d, treewy_dtype dtype);
+
+/*
+ * treewy_sample - one token from each row of logits, by given random numbers.
+ *   logits   [R, V] dtype, row_stride elements from row to row (any; a NaN counts as -inf)
+ *   u        [R] float32 in [0, 1)         the row's random number (values outside count as the nearest inside)
+ *   temperature [R] float32 or NULL (1)    at most 0 (or NaN): the first of the largest logits
+ *   top_k    [R] int32 or NULL             keep the top_k largest (at most 0: all)
+ *   top_p    [R] float32 or NULL           then the fewest of the largest whose likelihoods reach top_p of what is kept
+ *                                          (1 or more, or NaN: all; one token is always kept)
+ *   min_p    [R] float32 or NULL           likelihoods at least min_p of the largest (at most 0, or NaN: all)
+ *   token    [R] int32 written             -1 in a row without a value above -inf
+ *   logprob  [R] float32 written, or NULL  log of the token's likelihood, renormalised over the kept ones (-inf for -1)
+ *   err      [R] int32 or NULL             NO_TOKEN
+ * min_p and top_k act on the whole row, top_p on what both leave.  "Largest" goes by logit, equal ones by index.  The token is
+ * the first whose running sum of kept likelihoods, in the order of the vocabulary, passes u times their sum.
+ * A likelihood is held relative to the row's largest as floor(2^40 2^y), y = (logit - largest) (log2 e / temperature) with y
+ * and 2^y in float32, and all sums are whole numbers: the token depends on no order of summation.  top_p, u and min_p act
+ * as multiples of 2^-31 (2^-40), taken down.  1 <= V <= 2^20.
+ */
+treewy_status treewy_sample(const void *logits, int64_t row_stride, const float *u, const float *temperature,
+                            const int32_t *top_k, const float *top_p, const float *min_p, int R, int V, treewy_dtype dtype,
+                            int32_t *token, float *logprob, int32_t *err, void *stream);
+
+#ifdef __cplusplus
+}
+#endif
+
+#endif /* TREEWY_HYBRID_H */

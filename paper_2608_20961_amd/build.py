@@ -1,5 +1,5 @@
-"""Build libtreewy.so from csrc/ with hipcc for gfx950, and the Python binding's native call path (_binding.so, host
-code only) against the installed torch (both in-tree).
+"""Build libtreewy.so from csrc/ and csrc_hybrid/ with hipcc for gfx950, and the Python bindings' native call paths
+(_binding.so and _hybrid.so, host code only) against the installed torch (all in-tree).
 
     python -m paper_2608_20961_amd.build
 """
@@ -15,20 +15,24 @@ PKG = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(PKG)
 CSRC = os.path.join(PKG, "csrc")
 INCLUDE = os.path.join(ROOT, "include")
+CSRC_HYBRID = os.path.join(PKG, "csrc_hybrid")
 OBJDIR = os.path.join(ROOT, "_build")
 LIB = os.path.join(PKG, "libtreewy.so")
-BINDING = os.path.join(PKG, "_binding.so")
-SOURCES = ["api.hip", "verify.hip", "small.hip", "prefill.hip", "commit.hip", "snapshot.hip", "tree.hip"]
+BINDINGS = {os.path.join(PKG, "_binding.so"): os.path.join(CSRC, "binding.cpp"),
+            os.path.join(PKG, "_hybrid.so"): os.path.join(CSRC_HYBRID, "hybrid_binding.cpp")}
+SOURCES = [*(os.path.join(CSRC, n) for n in ("api.hip", "verify.hip", "small.hip", "prefill.hip", "commit.hip",
+                                             "snapshot.hip", "tree.hip")),
+           *(os.path.join(CSRC_HYBRID, n) for n in ("hybrid_api.hip", "append.hip", "attention.hip", "sample.hip"))]
 
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 FLAGS = ["--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-Wall",
          # no packed-fp32 instructions anywhere in the device code
          "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops",
-         "-I", INCLUDE, "-I", CSRC]
+         "-I", INCLUDE, "-I", CSRC, "-I", CSRC_HYBRID]
 
 
-def binding_command(obj: str) -> Optional[list]:
-    """g++ over binding.cpp (no device code) with torch's and HIP's headers; None where torch is not installed."""
+def binding_command(obj: str, source: str = os.path.join(CSRC, "binding.cpp")) -> Optional[list]:
+    """g++ over a binding (no device code) with torch's and HIP's headers; None where torch is not installed."""
     import sysconfig
 
     try:
@@ -40,28 +44,29 @@ def binding_command(obj: str) -> Optional[list]:
     inc = [*cpp_extension.include_paths(), sysconfig.get_paths()["include"], os.path.join(rocm, "include")]
     return ["g++", "-O2", "-std=c++17", "-fPIC", "-Wall", "-DUSE_ROCM=1", "-D__HIP_PLATFORM_AMD__=1",
             "-D_GLIBCXX_USE_CXX11_ABI=%d" % int(torch._C._GLIBCXX_USE_CXX11_ABI), *[x for i in inc for x in ("-isystem", i)],
-            "-I", INCLUDE, "-c", os.path.join(CSRC, "binding.cpp"), "-o", obj]
+            "-I", INCLUDE, "-c", source, "-o", obj]
 
 
-def link_binding(obj: str) -> None:
-    """Links the binding; torch's libraries and libtreewy.so are in the process when it is imported."""
+def link_binding(obj: str, to: str) -> None:
+    """Links a binding; torch's libraries and libtreewy.so are in the process when it is imported."""
     from torch.utils import cpp_extension
-    tmp = BINDING + ".tmp%d" % os.getpid()
+    tmp = to + ".tmp%d" % os.getpid()
     libs = [x for d in cpp_extension.library_paths() for x in ("-L", d, "-Wl,-rpath-link," + d)]
     subprocess.run(["g++", "-shared", "-fPIC", "-o", tmp, obj, "-L", PKG, "-Wl,-rpath,$ORIGIN", "-l:libtreewy.so", *libs,
                     "-ltorch_python", "-ltorch", "-ltorch_cpu", "-lc10", "-lc10_hip"], check=True)
-    os.replace(tmp, BINDING)
+    os.replace(tmp, to)
+
+
+def _object(source: str) -> str:
+    return os.path.join(OBJDIR, os.path.splitext(os.path.basename(source))[0] + ".o")
 
 
 def build(verbose: bool = False) -> str:
-    """Both libraries; where torch is not installed the C-ABI library alone."""
+    """All libraries; where torch is not installed the C-ABI library alone."""
     os.makedirs(OBJDIR, exist_ok=True)
-    objs = [os.path.join(OBJDIR, src.replace(".hip", ".o")) for src in SOURCES]
-    commands = {src: [HIPCC, *FLAGS, "-c", os.path.join(CSRC, src), "-o", obj] for src, obj in zip(SOURCES, objs)}
-    binding_obj = os.path.join(OBJDIR, "binding.o")
-    binding = binding_command(binding_obj)
-    if binding:
-        commands["binding.cpp"] = binding
+    commands = {src: [HIPCC, *FLAGS, "-c", src, "-o", _object(src)] for src in SOURCES}
+    bindings = {to: src for to, src in BINDINGS.items() if binding_command(_object(src), src)}
+    commands.update({src: binding_command(_object(src), src) for src in bindings.values()})
     procs = {}
     for src, cmd in commands.items():
         if verbose:
@@ -75,16 +80,16 @@ def build(verbose: bool = False) -> str:
             print(out, file=sys.stderr)
         if p.returncode:
             failed.append(src)
-    if set(failed) <= {"binding.cpp"}:                   # (the library does not depend on the binding)
+    if set(failed) <= set(BINDINGS.values()):            # (the library does not depend on the bindings)
         tmp = LIB + ".tmp%d" % os.getpid()
-        subprocess.run([HIPCC, "--offload-arch=gfx950", "-shared", "-fPIC", "-o", tmp, *objs], check=True)
+        subprocess.run([HIPCC, "--offload-arch=gfx950", "-shared", "-fPIC", "-o", tmp, *map(_object, SOURCES)], check=True)
         os.replace(tmp, LIB)
     if failed:
-        raise RuntimeError("the compiler failed on " + ", ".join(failed))
-    if binding:
-        link_binding(binding_obj)
-    else:
-        print("torch is not installed: built %s without the Python binding's native call path" % LIB, file=sys.stderr)
+        raise RuntimeError("the compiler failed on " + ", ".join(map(os.path.basename, failed)))
+    for to, src in bindings.items():
+        link_binding(_object(src), to)
+    if not bindings:
+        print("torch is not installed: built %s without the Python bindings' native call paths" % LIB, file=sys.stderr)
     return LIB
 
 

@@ -1,0 +1,87 @@
+// treewy_cache_append: a sequence's accepted path (or a prompt's tokens) into
+// its pages, keys rotated on the way.  One read and one write of every row
+// and nothing else, so a large call is bound by HBM and a small one by the
+// launch.  A thread owns two granules of 16 bytes of one (token, head): the
+// two halves of the same pairs where the head rotates, so that a rotated
+// granule is read once and its cosines and sines serve both.
+#include "hybrid_launch.h"
+#include "rotate.h"
+
+namespace treewy {
+
+namespace {
+
+template <typename T, int HD> __global__ __launch_bounds__(THREADS) void append_kernel(AppendArgs a, int blocks_per_seq) {
+    constexpr int E = Granule<T>::N, GRANULES = HD / E, LANES = GRANULES / 2;
+    const int b = blockIdx.x / blocks_per_seq, chunk = blockIdx.x - b * blocks_per_seq;
+    const int n0 = a.len[b], m = a.count ? a.count[b] : a.L;
+    // What holds for the whole sequence; every workgroup of it finds the same.
+    int flag = m < 0 || m > a.L ? TREEWY_FLAG_BAD_PATH : 0;
+    if (a.path && !flag) {
+        bool bad = false;
+        for (int l = threadIdx.x; l < m; l += THREADS) {
+            const int t = a.path[(int64_t)b * a.L + l], before = l ? a.path[(int64_t)b * a.L + l - 1] : -1;
+            bad |= t <= before || t >= a.N;
+        }
+        if (__syncthreads_or(bad)) flag = TREEWY_FLAG_BAD_PATH;
+    }
+    const int64_t room = min((int64_t)a.max_pages << a.log2_page, a.rot ? (int64_t)a.positions : INT64_MAX);
+    if (!flag && (n0 < 0 || (m > 0 && (int64_t)n0 + m > room))) flag = TREEWY_FLAG_CACHE_FULL;
+    if (chunk == 0 && threadIdx.x == 0) {
+        a.new_len[b] = flag ? n0 : n0 + m;
+        if (flag) flag_error(a.err, b, flag);
+    }
+    if (flag) return;
+
+    const int64_t item = (int64_t)chunk * THREADS + threadIdx.x;
+    const int lane = (int)(item % LANES);
+    const int64_t row = item / LANES;
+    const int l = (int)(row / a.H), h = (int)(row - (int64_t)l * a.H);
+    if (l >= m) return;
+    const int p = n0 + l, page = p >> a.log2_page;
+    const int id = a.table[(int64_t)b * a.max_pages + page];
+    if (id < 0 || id >= a.n_pages) {
+        if (lane == 0) flag_error(a.err, b, TREEWY_FLAG_BAD_PAGE);
+        return;
+    }
+    const int t = a.path ? a.path[(int64_t)b * a.L + l] : l;
+    const uint4 *k = reinterpret_cast<const uint4 *>((const T *)a.k + b * a.ks.seq + h * a.ks.head + t * a.ks.token);
+    const uint4 *v = reinterpret_cast<const uint4 *>((const T *)a.v + b * a.vs.seq + h * a.vs.head + t * a.vs.token);
+    const int64_t at = ((((int64_t)id * a.H + h) << a.log2_page) + (p & ((1 << a.log2_page) - 1))) * GRANULES;
+    uint4 *ko = (uint4 *)a.k_pages + at, *vo = (uint4 *)a.v_pages + at;
+
+    const int half = a.rot / (2 * E);                    // granules of the pairs' first halves
+    const bool turns = lane < half;
+    const int lo = turns ? lane : half + lane, hi = turns ? lane + half : lo + (GRANULES / 2 - half);
+    uint4 x = k[lo], y = k[hi];
+    const uint4 v0 = v[lo], v1 = v[hi];
+    if (turns) {
+        Angles<T> w;
+        w.load(a.cos, a.sin, (int64_t)p * (a.rot / 2), lane * E);
+        const uint4 first = rotated<T>(x, y, w, false);
+        y = rotated<T>(y, x, w, true);
+        x = first;
+    }
+    ko[lo] = x;
+    ko[hi] = y;
+    vo[lo] = v0;
+    vo[hi] = v1;
+}
+
+template <typename T> hipError_t launch(const AppendArgs &a, int d, hipStream_t stream) {
+    const int64_t items = (int64_t)a.L * a.H * (d / Granule<T>::N / 2);
+    const int64_t per_seq = items > THREADS ? (items + THREADS - 1) / THREADS : 1;
+    const dim3 grid((unsigned)(per_seq * a.B));
+    if (d == 64) hipLaunchKernelGGL((append_kernel<T, 64>), grid, dim3(THREADS), 0, stream, a, (int)per_seq);
+    else if (d == 128) hipLaunchKernelGGL((append_kernel<T, 128>), grid, dim3(THREADS), 0, stream, a, (int)per_seq);
+    else hipLaunchKernelGGL((append_kernel<T, 256>), grid, dim3(THREADS), 0, stream, a, (int)per_seq);
+    return hipGetLastError();
+}
+
+}  // namespace
+
+hipError_t launch_cache_append(const AppendArgs &a, int d, bool f32, hipStream_t stream) {
+    return f32 ? launch<float>(a, d, stream) : launch<__bf16>(a, d, stream);
+}
+
+}  // namespace treewy

@@ -1,0 +1,143 @@
+// C ABI of treewy_hybrid.h: host-side argument checks, then the launches on
+// the caller's stream.
+#include <stdint.h>
+
+#include "device.h"
+#include "hybrid_launch.h"
+
+namespace {
+
+bool aligned16(const void *p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
+
+treewy_status hip_status(hipError_t e) { return e == hipSuccess ? TREEWY_OK : TREEWY_ERR_HIP; }
+
+// Rows at 16-byte addresses: strides of dimensions longer than one.
+bool rows_aligned(const void *p, const treewy_strides &s, int seqs, int heads, int tokens, treewy_dtype dt) {
+    const int64_t e = dt == TREEWY_BF16 ? 8 : 4;
+    return aligned16(p) && (seqs <= 1 || s.seq % e == 0) && (heads <= 1 || s.head % e == 0) &&
+           (tokens <= 1 || s.token % e == 0);
+}
+
+// Largest |offset| of a row, in elements, stays within what 64 bits of bytes hold.
+bool strides_fit(const treewy_strides &s, int seqs, int heads, int tokens) {
+    const auto part = [](int64_t stride, int n) { return n > 1 ? (__int128)(stride < 0 ? -(__int128)stride : stride) * (n - 1) : 0; };
+    return part(s.seq, seqs) + part(s.head, heads) + part(s.token, tokens) < ((__int128)1 << 60);
+}
+
+treewy_status check_head(int d, treewy_dtype dt) {
+    if (dt != TREEWY_F32 && dt != TREEWY_BF16) return TREEWY_ERR_INVALID_ARG;
+    return d == 64 || d == 128 || d == 256 ? TREEWY_OK : TREEWY_ERR_UNSUPPORTED;
+}
+
+treewy_status check_rotation(const treewy_rotation *r, int d) {
+    if (!r) return TREEWY_OK;
+    if (r->dims < 0 || r->positions < 0) return TREEWY_ERR_INVALID_ARG;
+    if (r->dims == 0) return TREEWY_OK;
+    if (r->dims % 16 != 0 || r->dims > d) return TREEWY_ERR_UNSUPPORTED;
+    if (r->positions == 0 || !r->cos || !r->sin || !aligned16(r->cos) || !aligned16(r->sin)) return TREEWY_ERR_INVALID_ARG;
+    return TREEWY_OK;
+}
+
+treewy_status check_cache(const treewy_cache *c) {
+    if (!c || c->n_pages < 0 || c->max_pages < 0 || c->page_size <= 0) return TREEWY_ERR_INVALID_ARG;
+    if (c->page_size < 8 || c->page_size > 4096 || (c->page_size & (c->page_size - 1)) != 0) return TREEWY_ERR_UNSUPPORTED;
+    if ((int64_t)c->max_pages * c->page_size > (1 << 30)) return TREEWY_ERR_UNSUPPORTED;
+    if (!c->len || (c->max_pages > 0 && !c->page_table)) return TREEWY_ERR_INVALID_ARG;
+    if (c->n_pages > 0 && (!c->k || !c->v)) return TREEWY_ERR_INVALID_ARG;
+    return aligned16(c->k) && aligned16(c->v) ? TREEWY_OK : TREEWY_ERR_INVALID_ARG;
+}
+
+bool attention_sizes(int N, int B, int H_q, int H_kv, int d, treewy_dtype dt) {
+    return N >= 1 && N <= treewy::MAX_TREE && B >= 1 && H_kv >= 1 && H_q >= 1 && H_q % H_kv == 0 &&
+           check_head(d, dt) == TREEWY_OK && (int64_t)B * H_q * N <= INT32_MAX / 64;
+}
+
+}  // namespace
+
+extern "C" {
+
+treewy_status treewy_cache_append(const void *k, treewy_strides k_strides, const void *v, treewy_strides v_strides,
+                                  const treewy_cache *cache, const treewy_rotation *rotation, const int32_t *path, int L_max,
+                                  const int32_t *count, int N, int B, int H_kv, int d, treewy_dtype dtype, int32_t *new_len,
+                                  int32_t *err, void *stream) {
+    if (N < 0 || B < 0 || H_kv < 0 || L_max < 0) return TREEWY_ERR_INVALID_ARG;
+    treewy_status st = check_head(d, dtype);
+    if (st != TREEWY_OK) return st;
+    if (path ? N > treewy::MAX_TREE || L_max > treewy::MAX_TREE : L_max != N)
+        return path ? TREEWY_ERR_UNSUPPORTED : TREEWY_ERR_INVALID_ARG;
+    if (B == 0) return TREEWY_OK;
+    st = check_cache(cache);
+    if (st == TREEWY_OK) st = check_rotation(rotation, d);
+    if (st != TREEWY_OK) return st;
+    if (!new_len || new_len == cache->len) return TREEWY_ERR_INVALID_ARG;
+    if (N > 0 && L_max > 0 && H_kv > 0) {
+        if (!k || !v || !rows_aligned(k, k_strides, B, H_kv, N, dtype) || !rows_aligned(v, v_strides, B, H_kv, N, dtype) ||
+            !strides_fit(k_strides, B, H_kv, N) || !strides_fit(v_strides, B, H_kv, N))
+            return TREEWY_ERR_INVALID_ARG;
+    }
+    // (a workgroup per 256 pairs of granules, and one at least per sequence)
+    const int64_t per_seq = (int64_t)L_max * H_kv * (d * (dtype == TREEWY_BF16 ? 2 : 4) / 32) / 256 + 1;
+    if (per_seq * B > INT32_MAX) return TREEWY_ERR_UNSUPPORTED;
+    treewy::AppendArgs a{};
+    a.k = k, a.v = v, a.ks = k_strides, a.vs = v_strides;
+    a.k_pages = cache->k, a.v_pages = cache->v, a.table = cache->page_table, a.len = cache->len;
+    a.path = path, a.count = count, a.new_len = new_len, a.err = err;
+    if (rotation) a.cos = rotation->cos, a.sin = rotation->sin, a.positions = rotation->positions, a.rot = rotation->dims;
+    a.n_pages = cache->n_pages, a.max_pages = cache->max_pages, a.log2_page = __builtin_ctz((unsigned)cache->page_size);
+    a.L = L_max, a.N = N, a.B = B, a.H = H_kv;
+    return hip_status(treewy::launch_cache_append(a, d, dtype == TREEWY_F32, static_cast<hipStream_t>(stream)));
+}
+
+size_t treewy_tree_attention_workspace(int shared_len, int N, int B, int H_q, int H_kv, int d, treewy_dtype dtype) {
+    if (shared_len < 0 || !attention_sizes(N, B, H_q, H_kv, d, dtype)) return 0;
+    return treewy::tree_attention_workspace(shared_len, N, B, H_q, H_kv, d, dtype == TREEWY_F32);
+}
+
+treewy_status treewy_tree_attention(const void *q, treewy_strides q_strides, const void *k, treewy_strides k_strides,
+                                    const void *v, treewy_strides v_strides, const int32_t *parent, const treewy_cache *cache,
+                                    const treewy_rotation *rotation, int shared_len, float scale, int N, int B, int H_q,
+                                    int H_kv, int d, treewy_dtype dtype, void *o, treewy_strides o_strides, void *workspace,
+                                    size_t workspace_bytes, int32_t *err, void *stream) {
+    if (N < 0 || B < 0 || H_q < 0 || H_kv < 0 || shared_len < 0) return TREEWY_ERR_INVALID_ARG;
+    treewy_status st = check_head(d, dtype);
+    if (st != TREEWY_OK) return st;
+    if (N > treewy::MAX_TREE) return TREEWY_ERR_UNSUPPORTED;
+    if (N == 0 || B == 0 || H_q == 0) return TREEWY_OK;
+    if (H_kv == 0 || H_q % H_kv != 0) return TREEWY_ERR_INVALID_ARG;
+    if (!attention_sizes(N, B, H_q, H_kv, d, dtype)) return TREEWY_ERR_UNSUPPORTED;
+    st = check_cache(cache);
+    if (st == TREEWY_OK) st = check_rotation(rotation, d);
+    if (st != TREEWY_OK) return st;
+    if (!q || !k || !v || !o) return TREEWY_ERR_INVALID_ARG;
+    if (!rows_aligned(q, q_strides, B, H_q, N, dtype) || !rows_aligned(k, k_strides, B, H_kv, N, dtype) ||
+        !rows_aligned(v, v_strides, B, H_kv, N, dtype) || !rows_aligned(o, o_strides, B, H_q, N, dtype) ||
+        !strides_fit(q_strides, B, H_q, N) || !strides_fit(k_strides, B, H_kv, N) || !strides_fit(v_strides, B, H_kv, N) ||
+        !strides_fit(o_strides, B, H_q, N))
+        return TREEWY_ERR_INVALID_ARG;
+    const bool f32 = dtype == TREEWY_F32;
+    const size_t need = treewy::tree_attention_workspace(shared_len, N, B, H_q, H_kv, d, f32);
+    if (need > 0 && (!workspace || !aligned16(workspace) || workspace_bytes < need)) return TREEWY_ERR_INVALID_ARG;
+    treewy::AttendArgs a{};
+    a.q = q, a.k = k, a.v = v, a.qs = q_strides, a.ks = k_strides, a.vs = v_strides, a.os = o_strides;
+    a.parent = parent, a.k_pages = cache->k, a.v_pages = cache->v, a.table = cache->page_table, a.len = cache->len;
+    if (rotation) a.cos = rotation->cos, a.sin = rotation->sin, a.positions = rotation->positions, a.rot = rotation->dims;
+    a.o = o, a.err = err;
+    a.n_pages = cache->n_pages, a.max_pages = cache->max_pages, a.log2_page = __builtin_ctz((unsigned)cache->page_size);
+    a.shared = shared_len, a.N = N, a.B = B, a.H_q = H_q, a.H_kv = H_kv, a.scale = scale;
+    return hip_status(treewy::launch_tree_attention(a, d, f32, workspace, static_cast<hipStream_t>(stream)));
+}
+
+treewy_status treewy_sample(const void *logits, int64_t row_stride, const float *u, const float *temperature,
+                            const int32_t *top_k, const float *top_p, const float *min_p, int R, int V, treewy_dtype dtype,
+                            int32_t *token, float *logprob, int32_t *err, void *stream) {
+    if (R < 0 || V < 0) return TREEWY_ERR_INVALID_ARG;
+    if (dtype != TREEWY_F32 && dtype != TREEWY_BF16) return TREEWY_ERR_INVALID_ARG;
+    if (V > (1 << 20)) return TREEWY_ERR_UNSUPPORTED;
+    if (R == 0) return TREEWY_OK;
+    if (V == 0 || !logits || !u || !token) return TREEWY_ERR_INVALID_ARG;
+    if (reinterpret_cast<uintptr_t>(logits) % (dtype == TREEWY_BF16 ? 2 : 4) != 0) return TREEWY_ERR_INVALID_ARG;
+    treewy::SampleArgs a{logits, row_stride, u, temperature, top_p, min_p, top_k, R, V, token, err, logprob};
+    return hip_status(treewy::launch_sample(a, dtype == TREEWY_F32, static_cast<hipStream_t>(stream)));
+}
+
+}  // extern "C"

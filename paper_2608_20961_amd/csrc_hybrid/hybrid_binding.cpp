@@ -1,0 +1,256 @@
+// Native call path of hybrid.py: one call checks every tensor, allocates the
+// outputs and the workspace that were not given, takes the current stream and
+// calls the C ABI of treewy_hybrid.h.
+//
+// Each function returns the call's result when everything is as the library
+// wants it, the status (an int) when the library refused the call, and None
+// when any argument is not plainly acceptable; the caller then repeats the
+// call through Python, whose checks say what is wrong.
+#include <torch/csrc/autograd/python_variable.h>
+
+#include <ATen/ATen.h>
+#include <ATen/TensorSubclassLikeUtils.h>
+#include <c10/hip/HIPFunctions.h>
+#include <c10/hip/HIPStream.h>
+
+#include "treewy_hybrid.h"
+
+namespace {
+
+using at::Tensor;
+
+struct Refused {};                                       // -> None
+
+constexpr at::ScalarType F32 = at::kFloat, I32 = at::kInt;
+
+// A plain strided GPU tensor on device `d`.
+const Tensor &plain(PyObject *x, int d) {
+    if (!THPVariable_CheckExact(x)) throw Refused{};
+    const Tensor &t = THPVariable_Unpack(x);
+    if (!t.defined() || t.layout() != at::kStrided || !t.device().is_cuda() || t.device().index() != d || !t.has_storage() ||
+        at::isTensorSubclassLike(t))
+        throw Refused{};
+    return t;
+}
+
+// ... of this type and shape, contiguous
+const Tensor &dense(PyObject *x, int d, at::ScalarType type, at::IntArrayRef shape) {
+    const Tensor &t = plain(x, d);
+    if (t.scalar_type() != type || t.sizes() != shape || !t.is_contiguous()) throw Refused{};
+    return t;
+}
+
+void *dense_or_null(PyObject *x, int d, at::ScalarType type, at::IntArrayRef shape) {
+    return x == Py_None ? nullptr : dense(x, d, type, shape).data_ptr();
+}
+
+Tensor made(PyObject *x, int d, at::ScalarType type, at::IntArrayRef shape) {
+    if (x != Py_None) return dense(x, d, type, shape);
+    return at::empty(shape, at::TensorOptions().dtype(type).device(at::kCUDA, d));
+}
+
+// [B, heads, N, d] whose last dimension is contiguous, rows at multiples of 16 bytes
+const Tensor &rows(PyObject *x, int d, at::ScalarType type, at::IntArrayRef shape) {
+    const Tensor &t = plain(x, d);
+    if (t.scalar_type() != type || t.sizes() != shape || (t.size(3) > 1 && t.stride(3) != 1)) throw Refused{};
+    const int64_t e = 16 / (int64_t)t.element_size();
+    if (reinterpret_cast<uintptr_t>(t.data_ptr()) % 16) throw Refused{};
+    for (int i = 0; i < 3; ++i)
+        if (t.size(i) > 1 && t.stride(i) % e) throw Refused{};
+    return t;
+}
+
+treewy_strides strides(const Tensor &t) { return {t.stride(0), t.stride(1), t.stride(2)}; }
+
+treewy_dtype type_of(const Tensor &t) {
+    if (t.scalar_type() == at::kBFloat16) return TREEWY_BF16;
+    if (t.scalar_type() == at::kFloat) return TREEWY_F32;
+    throw Refused{};
+}
+
+int64_t size(const Tensor &t, int dims, int i) {
+    if (t.dim() != dims || t.size(i) > INT32_MAX) throw Refused{};
+    return t.size(i);
+}
+
+void *stream_of(PyObject *s, int d) {
+    if (s == Py_None) return c10::hip::getCurrentHIPStream((c10::DeviceIndex)d).stream();
+    PyObject *h = PyObject_GetAttrString(s, "cuda_stream");
+    void *p = h ? PyLong_AsVoidPtr(h) : nullptr;
+    Py_XDECREF(h);
+    if (PyErr_Occurred()) {
+        PyErr_Clear();
+        throw Refused{};
+    }
+    return p;
+}
+
+// The cache's tensors: k_pages, v_pages, page_table, cache_len from a[i] on.
+treewy_cache cache_of(PyObject *const *a, int d, at::ScalarType type, int64_t B, int64_t H, int64_t D) {
+    const Tensor &k = plain(a[0], d), &table = plain(a[2], d);
+    const int64_t n = size(k, 4, 0), page = size(k, 4, 2), width = size(table, 2, 1);
+    dense(a[0], d, type, {n, H, page, D});
+    const Tensor &v = dense(a[1], d, type, {n, H, page, D});
+    dense(a[2], d, I32, {B, width});
+    const Tensor &len = dense(a[3], d, I32, {B});
+    return {k.data_ptr(), v.data_ptr(), (const int32_t *)table.data_ptr(), (const int32_t *)len.data_ptr(), (int)n, (int)width, (int)page};
+}
+
+treewy_rotation rotation_of(PyObject *c, PyObject *s, int d) {
+    if (c == Py_None && s == Py_None) return {nullptr, nullptr, 0, 0};
+    const Tensor &cos = plain(c, d);
+    const int64_t n = size(cos, 2, 0), half = size(cos, 2, 1);
+    if (half > INT32_MAX / 2) throw Refused{};
+    dense(c, d, F32, {n, half});
+    const Tensor &sin = dense(s, d, F32, {n, half});
+    return {(const float *)cos.data_ptr(), (const float *)sin.data_ptr(), (int)n, (int)(2 * half)};
+}
+
+// What the call returns, wrapped before the launch: past the launch nothing can fail.
+struct Result {
+    PyObject *r = nullptr;
+    explicit Result(std::initializer_list<Tensor> out) {
+        r = out.size() == 1 ? THPVariable_Wrap(*out.begin()) : PyTuple_New((Py_ssize_t)out.size());
+        if (!r) throw Refused{};
+        Py_ssize_t i = 0;
+        if (out.size() > 1)
+            for (const Tensor &t : out) {
+                PyObject *x = THPVariable_Wrap(t);
+                if (!x) {
+                    Py_CLEAR(r);
+                    throw Refused{};
+                }
+                PyTuple_SET_ITEM(r, i++, x);
+            }
+    }
+    Result(const Result &) = delete;
+    ~Result() { Py_XDECREF(r); }
+    PyObject *after(treewy_status st) {
+        if (st != TREEWY_OK) return PyLong_FromLong(st);
+        PyObject *x = r;
+        r = nullptr;
+        return x;
+    }
+};
+
+// f(current device); None where it threw (nothing is launched then).
+template <typename F> PyObject *guarded(Py_ssize_t n, Py_ssize_t want, F &&f) {
+    if (n != want) {
+        PyErr_SetString(PyExc_TypeError, "wrong number of arguments");
+        return nullptr;
+    }
+    try {
+        return f((int)c10::hip::current_device());
+    } catch (...) {
+        PyErr_Clear();
+        Py_RETURN_NONE;
+    }
+}
+
+// The C call without the interpreter lock; every pointer is taken before.
+template <typename F> treewy_status unlocked(F &&f) {
+    struct Unlocked {
+        PyThreadState *state = PyEval_SaveThread();
+        ~Unlocked() { PyEval_RestoreThread(state); }
+    } lock;
+    return f();
+}
+
+// k, v, k_pages, v_pages, page_table, cache_len, cos, sin, path, count, new_len, err, stream -> new_len
+PyObject *cache_append(PyObject *, PyObject *const *a, Py_ssize_t n) {
+    return guarded(n, 13, [&](int d) {
+        const Tensor &k = plain(a[0], d);
+        const int64_t B = size(k, 4, 0), H = size(k, 4, 1), N = size(k, 4, 2), D = size(k, 4, 3);
+        const auto type = k.scalar_type();
+        const treewy_dtype dt = type_of(k);
+        rows(a[0], d, type, {B, H, N, D});
+        const Tensor &v = rows(a[1], d, type, {B, H, N, D});
+        const treewy_cache cache = cache_of(a + 2, d, type, B, H, D);
+        const treewy_rotation rot = rotation_of(a[6], a[7], d);
+        int64_t L = N;
+        const int32_t *path = nullptr;
+        if (a[8] != Py_None) {
+            L = size(plain(a[8], d), 2, 1);
+            path = (const int32_t *)dense(a[8], d, I32, {B, L}).data_ptr();
+        }
+        void *count = dense_or_null(a[9], d, I32, {B}), *err = dense_or_null(a[11], d, I32, {B}), *s = stream_of(a[12], d);
+        const Tensor new_len = made(a[10], d, I32, {B});
+        void *kp = k.data_ptr(), *vp = v.data_ptr(), *out = new_len.data_ptr();
+        const treewy_strides ks = strides(k), vs = strides(v);
+        Result result({new_len});
+        return result.after(unlocked([&] {
+            return treewy_cache_append(kp, ks, vp, vs, &cache, &rot, path, (int)L, (const int32_t *)count, (int)N, (int)B, (int)H,
+                                       (int)D, dt, (int32_t *)out, (int32_t *)err, s);
+        }));
+    });
+}
+
+// q, k, v, parent, k_pages, v_pages, page_table, cache_len, cos, sin, shared_len, scale, o, workspace, err, stream -> o
+PyObject *tree_attention(PyObject *, PyObject *const *a, Py_ssize_t n) {
+    return guarded(n, 16, [&](int d) {
+        const Tensor &q = plain(a[0], d), &k = plain(a[1], d);
+        const int64_t B = size(q, 4, 0), Hq = size(q, 4, 1), N = size(q, 4, 2), D = size(q, 4, 3), H = size(k, 4, 1);
+        const auto type = q.scalar_type();
+        const treewy_dtype dt = type_of(q);
+        rows(a[0], d, type, {B, Hq, N, D});
+        rows(a[1], d, type, {B, H, N, D});
+        const Tensor &v = rows(a[2], d, type, {B, H, N, D});
+        void *parent = dense_or_null(a[3], d, I32, {B, N});
+        const treewy_cache cache = cache_of(a + 4, d, type, B, H, D);
+        const treewy_rotation rot = rotation_of(a[8], a[9], d);
+        int overflow = 0;
+        if (!PyLong_CheckExact(a[10]) || !PyFloat_CheckExact(a[11])) throw Refused{};
+        const long shared = PyLong_AsLongAndOverflow(a[10], &overflow);
+        if (overflow || shared < 0 || shared > INT32_MAX) throw Refused{};
+        const float scale = (float)PyFloat_AS_DOUBLE(a[11]);
+        void *err = dense_or_null(a[14], d, I32, {B}), *s = stream_of(a[15], d);
+        const Tensor o = a[12] == Py_None ? at::empty({B, Hq, N, D}, q.options()) : rows(a[12], d, type, {B, Hq, N, D});
+        const size_t need = treewy_tree_attention_workspace((int)shared, (int)N, (int)B, (int)Hq, (int)H, (int)D, dt);
+        Tensor ws;
+        if (a[13] != Py_None) {
+            ws = plain(a[13], d);
+            if (ws.scalar_type() != at::kByte || ws.dim() != 1 || !ws.is_contiguous()) throw Refused{};
+        } else {
+            if (a[15] != Py_None) throw Refused{};       // (of the current stream's pool: Python takes it from the given one's)
+            ws = at::empty({(int64_t)need}, q.options().dtype(at::kByte));
+        }
+        const int64_t bytes = ws.numel();
+        void *qp = q.data_ptr(), *kp = k.data_ptr(), *vp = v.data_ptr(), *op = o.data_ptr(), *wp = bytes ? ws.data_ptr() : nullptr;
+        const treewy_strides qs = strides(q), ks = strides(k), vs = strides(v), os = strides(o);
+        Result result({o});
+        return result.after(unlocked([&] {
+            return treewy_tree_attention(qp, qs, kp, ks, vp, vs, (const int32_t *)parent, &cache, &rot, (int)shared, scale, (int)N,
+                                         (int)B, (int)Hq, (int)H, (int)D, dt, op, os, wp, (size_t)bytes, (int32_t *)err, s);
+        }));
+    });
+}
+
+// logits, u, temperature, top_k, top_p, min_p, token, logprob, err, stream -> (token, logprob)
+PyObject *sample(PyObject *, PyObject *const *a, Py_ssize_t n) {
+    return guarded(n, 10, [&](int d) {
+        const Tensor &x = plain(a[0], d);
+        const int64_t R = size(x, 2, 0), V = size(x, 2, 1);
+        const treewy_dtype dt = type_of(x);
+        if (V > 1 && x.stride(1) != 1) throw Refused{};
+        const int64_t stride = x.stride(0);
+        void *u = dense(a[1], d, F32, {R}).data_ptr();
+        void *t = dense_or_null(a[2], d, F32, {R}), *k = dense_or_null(a[3], d, I32, {R}), *p = dense_or_null(a[4], d, F32, {R}),
+             *m = dense_or_null(a[5], d, F32, {R}), *err = dense_or_null(a[8], d, I32, {R}), *s = stream_of(a[9], d);
+        const Tensor token = made(a[6], d, I32, {R}), logprob = made(a[7], d, F32, {R});
+        void *xp = x.data_ptr(), *tp = token.data_ptr(), *lp = logprob.data_ptr();
+        Result result({token, logprob});
+        return result.after(unlocked([&] {
+            return treewy_sample(xp, stride, (const float *)u, (const float *)t, (const int32_t *)k, (const float *)p, (const float *)m,
+                                 (int)R, (int)V, dt, (int32_t *)tp, (float *)lp, (int32_t *)err, s);
+        }));
+    });
+}
+
+#define TREEWY_METHOD(f) {#f, (PyCFunction)(void (*)(void))f, METH_FASTCALL, nullptr}
+PyMethodDef methods[] = {TREEWY_METHOD(cache_append), TREEWY_METHOD(tree_attention), TREEWY_METHOD(sample),
+                         {nullptr, nullptr, 0, nullptr}};
+PyModuleDef module = {PyModuleDef_HEAD_INIT, "_hybrid", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
+
+}  // namespace
+
+PyMODINIT_FUNC PyInit__hybrid() { return PyModule_Create(&module); }

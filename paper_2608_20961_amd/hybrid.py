@@ -1,0 +1,203 @@
+"""Python binding of what treewy_hybrid.h declares: the softmax side of a gated-delta hybrid's decode round.
+
+Argument marshalling only, as in treewy.py: every computation runs in the HIP kernels of libtreewy.so, there is no CPU
+fallback, and importing this module raises if the library has not been built.  Calls go through a native path
+(csrc_hybrid/hybrid_binding.cpp); one that it does not take runs through the checks here, which name what is wrong.
+
+Function names match the C ABI, whose header says what each computes:
+  treewy_cache_append(k, v, k_pages, v_pages, page_table, cache_len, ...) -> new_len
+  treewy_tree_attention(q, k, v, parent, k_pages, v_pages, page_table, cache_len, ...) -> o
+  treewy_sample(logits, u, ...) -> (token, logprob)
+
+Shapes, with B sequences, H_q query heads over H_kv key heads of d values (64, 128 or 256), N draft nodes or tokens:
+  q, o [B, H_q, N, d] and k, v [B, H_kv, N, d], bfloat16 or float32, the last dimension contiguous, the others any strides that
+  put rows at multiples of 16 bytes (so a [B, N, heads, d] projection needs only .transpose(1, 2));
+  k_pages, v_pages [n_pages, H_kv, page_size, d] of the same type, page_table [B, max_pages] and cache_len [B] int32;
+  cos, sin [positions, dims / 2] float32: the first `dims` values of a head rotate (None: none).
+
+    o = treewy_tree_attention(q, k, v, parent, k_pages, v_pages, page_table, cache_len, cos=cos, sin=sin)
+    token, logprob = treewy_sample(logits.view(B * N, V), u, temperature=t, top_p=p)
+    path, path_len, bonus = treewy.treewy_accept_greedy(parent, draft_token, token.view(B, N), root_token, L_max)
+    cache_len = treewy_cache_append(k, v, k_pages, v_pages, page_table, cache_len, cos=cos, sin=sin, path=path, count=path_len)
+"""
+from __future__ import annotations
+
+import ctypes
+import types
+import warnings
+from typing import Tuple
+
+import torch
+
+from .treewy import _I, _P, TREEWY_BF16, TREEWY_F32, TreewyError, _check, _need, _ptr, _stream, _taken, lib  # noqa: F401
+
+try:
+    from . import _hybrid  # (after the library it calls)
+except ImportError as e:
+    warnings.warn("the native call path of the hybrid calls does not load (%s): every call runs through the slower Python "
+                  "checks; `python -m paper_2608_20961_amd.build` builds it against the installed torch" % e, RuntimeWarning)
+    _hybrid = types.SimpleNamespace(**dict.fromkeys(("cache_append", "tree_attention", "sample"), lambda *a: None))
+
+FLAG_BAD_PAGE, FLAG_CACHE_FULL, FLAG_NO_TOKEN = 4, 8, 16
+
+
+class Strides(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int64) for n in ("seq", "head", "token")]
+
+
+class Cache(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_void_p) for n in ("k", "v", "page_table", "len")] + [(n, _I) for n in ("n_pages", "max_pages", "page_size")]
+
+
+class Rotation(ctypes.Structure):
+    _fields_ = [("cos", ctypes.c_void_p), ("sin", ctypes.c_void_p), ("positions", _I), ("dims", _I)]
+
+
+_CP, _RP = ctypes.POINTER(Cache), ctypes.POINTER(Rotation)
+lib.treewy_cache_append.argtypes = [_P, Strides, _P, Strides, _CP, _RP, _P, _I, _P] + [_I] * 5 + [_P] * 3
+lib.treewy_cache_append.restype = _I
+lib.treewy_tree_attention.argtypes = ([_P, Strides] * 3 + [_P, _CP, _RP, _I, ctypes.c_float] + [_I] * 6 +
+                                      [_P, Strides, _P, ctypes.c_size_t, _P, _P])
+lib.treewy_tree_attention.restype = _I
+lib.treewy_tree_attention_workspace.argtypes = [_I] * 7
+lib.treewy_tree_attention_workspace.restype = ctypes.c_size_t
+lib.treewy_sample.argtypes = [_P, ctypes.c_int64] + [_P] * 5 + [_I] * 3 + [_P] * 4
+lib.treewy_sample.restype = _I
+
+EXPORTED = ("treewy_cache_append", "treewy_tree_attention", "treewy_tree_attention_workspace", "treewy_sample")
+
+
+def _dtype(t: torch.Tensor, name: str) -> int:
+    if not isinstance(t, torch.Tensor):
+        raise TypeError("%s must be a torch.Tensor" % name)
+    if t.dtype not in (torch.bfloat16, torch.float32):
+        raise TypeError("%s must be bfloat16 or float32, got %s" % (name, t.dtype))
+    return TREEWY_BF16 if t.dtype == torch.bfloat16 else TREEWY_F32
+
+
+def _dims(t, name: str, n: int) -> tuple:
+    if not isinstance(t, torch.Tensor):
+        raise TypeError("%s must be a torch.Tensor" % name)
+    if t.dim() != n:
+        raise ValueError("%s must have %d dimensions, got shape %s" % (name, n, tuple(t.shape)))
+    return tuple(t.shape)
+
+
+def _rows(t, name: str, dtype, shape) -> Strides:
+    """Checks [B, heads, N, d] rows at multiples of 16 bytes, and gives their strides."""
+    if _dims(t, name, 4) != tuple(shape):
+        raise ValueError("%s must have shape %s, got %s" % (name, tuple(shape), tuple(t.shape)))
+    _need(t.reshape(-1)[:0] if t.is_contiguous() else t[:0].contiguous().reshape(-1), name, dtype, (0,))  # (type and device)
+    e = 16 // t.element_size()
+    if t.numel() and (t.shape[3] > 1 and t.stride(3) != 1 or t.data_ptr() % 16 or
+                      any(n > 1 and s % e for n, s in zip(t.shape[:3], t.stride()[:3]))):
+        raise ValueError("%s must have contiguous rows at multiples of 16 bytes, got strides %s" % (name, t.stride()))
+    return Strides(*t.stride()[:3])
+
+
+def _optional(t, name: str, dtype, shape):
+    if t is not None:
+        _need(t, name, dtype, shape)
+    return _ptr(t)
+
+
+def _cache(k_pages, v_pages, page_table, cache_len, dtype, B: int, H: int, d: int) -> Cache:
+    n, _, page, _ = _dims(k_pages, "k_pages", 4)
+    width = _dims(page_table, "page_table", 2)[1]
+    _need(k_pages, "k_pages", dtype, (n, H, page, d)); _need(v_pages, "v_pages", dtype, (n, H, page, d))
+    _need(page_table, "page_table", torch.int32, (B, width)); _need(cache_len, "cache_len", torch.int32, (B,))
+    return Cache(k_pages.data_ptr(), v_pages.data_ptr(), page_table.data_ptr(), cache_len.data_ptr(), n, width, page)
+
+
+def _rotation(cos, sin) -> Rotation:
+    if cos is None and sin is None:
+        return Rotation(None, None, 0, 0)
+    if cos is None or sin is None:
+        raise ValueError("cos and sin come together")
+    n, half = _dims(cos, "cos", 2)
+    _need(cos, "cos", torch.float32, (n, half)); _need(sin, "sin", torch.float32, (n, half))
+    return Rotation(cos.data_ptr(), sin.data_ptr(), n, 2 * half)
+
+
+def treewy_cache_append(k, v, k_pages, v_pages, page_table, cache_len, cos=None, sin=None, path=None, count=None, new_len=None,
+                        err=None, stream=None) -> torch.Tensor:
+    """Rotates keys to positions cache_len, cache_len + 1, ... and writes them and the values into the pages, in place: the
+    nodes of `path` [B, L_max] (the first `count` [B] of them), or without one the first `count` tokens (all by default).
+    Returns the new lengths; cache_len itself is left as it is."""
+    r = _hybrid.cache_append(k, v, k_pages, v_pages, page_table, cache_len, cos, sin, path, count, new_len, err, stream)
+    if _taken(r, "treewy_cache_append"):
+        return r
+    B, H, N, d = _dims(k, "k", 4)
+    dt = _dtype(k, "k")
+    ks, vs = _rows(k, "k", k.dtype, (B, H, N, d)), _rows(v, "v", k.dtype, (B, H, N, d))
+    cache = _cache(k_pages, v_pages, page_table, cache_len, k.dtype, B, H, d)
+    rot = _rotation(cos, sin)
+    L = N if path is None else _dims(path, "path", 2)[1]
+    p, c, e = _optional(path, "path", torch.int32, (B, L)), _optional(count, "count", torch.int32, (B,)), _optional(err, "err", torch.int32, (B,))
+    if new_len is None:
+        new_len = torch.empty((B,), dtype=torch.int32, device=k.device)
+    _need(new_len, "new_len", torch.int32, (B,))
+    _check(lib.treewy_cache_append(_ptr(k), ks, _ptr(v), vs, ctypes.byref(cache), ctypes.byref(rot), p, L, c, N, B, H, d, dt,
+                                   _ptr(new_len), e, _stream(stream)), "treewy_cache_append")
+    return new_len
+
+
+def treewy_tree_attention(q, k, v, parent, k_pages, v_pages, page_table, cache_len, cos=None, sin=None, shared_len: int = 0,
+                          scale=None, o=None, workspace=None, err=None, stream=None) -> torch.Tensor:
+    """Attention of every draft node over the cached context, its ancestors and itself (parent None: a chain; N = 1: plain
+    decoding).  `scale` is 1 / sqrt(d) by default.  `workspace` is a uint8 tensor of at least
+    lib.treewy_tree_attention_workspace(...) bytes; without one the call takes it from PyTorch."""
+    if scale is None and isinstance(q, torch.Tensor) and q.dim() == 4:
+        scale = max(q.shape[3], 1) ** -0.5
+    r = _hybrid.tree_attention(q, k, v, parent, k_pages, v_pages, page_table, cache_len, cos, sin, shared_len, scale, o, workspace,
+                               err, stream)
+    if _taken(r, "treewy_tree_attention"):
+        return r
+    B, Hq, N, d = _dims(q, "q", 4)
+    H = _dims(k, "k", 4)[1]
+    dt = _dtype(q, "q")
+    qs, ks, vs = _rows(q, "q", q.dtype, (B, Hq, N, d)), _rows(k, "k", q.dtype, (B, H, N, d)), _rows(v, "v", q.dtype, (B, H, N, d))
+    p = _optional(parent, "parent", torch.int32, (B, N))
+    cache = _cache(k_pages, v_pages, page_table, cache_len, q.dtype, B, H, d)
+    rot = _rotation(cos, sin)
+    e = _optional(err, "err", torch.int32, (B,))
+    shared_len, scale = int(shared_len), float(scale)
+    if not 0 <= shared_len < 1 << 31:
+        raise ValueError("shared_len must be a length, got %d" % shared_len)
+    if o is None:
+        o = torch.empty((B, Hq, N, d), dtype=q.dtype, device=q.device)
+    os_ = _rows(o, "o", q.dtype, (B, Hq, N, d))
+    if workspace is None:
+        need = lib.treewy_tree_attention_workspace(shared_len, N, B, Hq, H, d, dt)
+        with torch.cuda.stream(stream):                  # (memory that this stream's later work may have again, no other's)
+            workspace = torch.empty((need,), dtype=torch.uint8, device=q.device)
+    _need(workspace, "workspace", torch.uint8, (workspace.numel(),))
+    _check(lib.treewy_tree_attention(_ptr(q), qs, _ptr(k), ks, _ptr(v), vs, p, ctypes.byref(cache), ctypes.byref(rot), shared_len,
+                                     scale, N, B, Hq, H, d, dt, _ptr(o), os_, _ptr(workspace) if workspace.numel() else None,
+                                     workspace.numel(), e, _stream(stream)), "treewy_tree_attention")
+    return o
+
+
+def treewy_sample(logits, u, temperature=None, top_k=None, top_p=None, min_p=None, token=None, logprob=None, err=None,
+                  stream=None) -> Tuple[torch.Tensor, torch.Tensor]:
+    """One token of each row of logits [R, V] (bfloat16 or float32, rows contiguous, any distance apart) by the random numbers
+    u [R], and the log of its likelihood among the kept tokens.  temperature, top_p, min_p [R] float32, top_k [R] int32."""
+    r = _hybrid.sample(logits, u, temperature, top_k, top_p, min_p, token, logprob, err, stream)
+    if _taken(r, "treewy_sample"):
+        return r
+    R, V = _dims(logits, "logits", 2)
+    dt = _dtype(logits, "logits")
+    if V > 1 and logits.stride(1) != 1:
+        raise ValueError("logits must have contiguous rows, got strides %s" % (logits.stride(),))
+    _need(logits[:0].contiguous(), "logits", logits.dtype, (0, V))                                       # (type and device)
+    _need(u, "u", torch.float32, (R,))
+    t, p, m = (_optional(x, n, torch.float32, (R,)) for x, n in ((temperature, "temperature"), (top_p, "top_p"), (min_p, "min_p")))
+    k, e = _optional(top_k, "top_k", torch.int32, (R,)), _optional(err, "err", torch.int32, (R,))
+    if token is None:
+        token = torch.empty((R,), dtype=torch.int32, device=logits.device)
+    if logprob is None:
+        logprob = torch.empty((R,), dtype=torch.float32, device=logits.device)
+    _need(token, "token", torch.int32, (R,)); _need(logprob, "logprob", torch.float32, (R,))
+    _check(lib.treewy_sample(_ptr(logits), logits.stride(0), _ptr(u), t, k, p, m, R, V, dt, _ptr(token), _ptr(logprob), e,
+                             _stream(stream)), "treewy_sample")
+    return token, logprob
