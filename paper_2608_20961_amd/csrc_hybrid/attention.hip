@@ -16,12 +16,16 @@
 // by sequence), of which every workgroup takes an equal, consecutive part,
 // however ragged the lengths.  A row tile ("unit") that one workgroup has
 // whole is written at once; the parts of others go to the workspace and are
-// joined by a second launch.  Which part a workgroup has follows from the
-// lengths, which only the device knows, so that no call waits for them.
+// joined by a last launch.  A first launch finds, from the lengths that only
+// the device knows, where every workgroup begins, and makes the draft's own
+// keys and values the like of a cached page: rotated, in rows one after the
+// other, with the ancestors' bits beside them.
 #include "hybrid_launch.h"
 #include "launch.h"
 #include "mfma16.h"
 #include "rotate.h"
+
+#include <type_traits>
 
 namespace treewy {
 
@@ -39,16 +43,20 @@ __device__ __forceinline__ f32x16 mma_f32(float a, float b, f32x16 c) {
     return __builtin_amdgcn_mfma_f32_32x32x2f32(a, b, c, 0, 0, 0);
 }
 
-// Tile and wave shape of a kernel: T and head size, row groups, key groups, keys of a tile.
-template <typename T_, int HD_, int WR_, int WK_, int KT_> struct Shape {
+// Tile and wave shape of a kernel: T and head size, row groups, key groups, keys of a tile, 16-byte steps of a row that may
+// rotate.  A rotated bf16 query is held as two bf16 (rounding it once moved scores by 2^-9 of their size, as much as all the
+// other roundings together); what does not rotate is exact.
+template <typename T_, int HD_, int WR_, int WK_, int KT_, int TURN_> struct Shape {
     using T = T_;
     static constexpr int HD = HD_, WR = WR_, WK = WK_, KT = KT_;
     static constexpr int RT = 32 * WR, NT = 64 * WR * WK, WAVES = WR * WK;
     static constexpr int E = 16 / (int)sizeof(T), GRAN = HD / E, STEPS = GRAN / 2, DT = HD / 32;
+    static constexpr int TURN = TURN_, LO = sizeof(T) == 2 ? TURN : 0;
     static constexpr int TILE = KT * GRAN;               // granules of a tile's keys (and of its values)
     static constexpr int LOADS = TILE / 64;              // wave-wide loads of them
     static_assert(KT % (32 * WK) == 0 && LOADS % WAVES == 0, "every wave has as much");
     static_assert((WK - 1) * WR * 32 * HD * 4 <= 2 * TILE * 16, "key groups meet in one tile's LDS");
+    static_assert(128 % KT == 0, "shared keys end with a tile");
 };
 
 // Where granule g of row r stands in its LDS row: the sixteen lanes that a
@@ -75,81 +83,37 @@ __host__ __device__ inline int draft_tiles_of(int unit, int RT, int KT, int G, i
     return ((last < N ? last : N - 1) + KT) / KT;        // nodes after a row tile's last are nobody's ancestors in it
 }
 
+// Where a workgroup begins in the list, and how many tiles it has.
+struct Start {
+    int b, h, rt, t0, tiles, pad[3];                     // b = -1: shared keys, rt among a head's shared units
+};
+
+// What the first launch leaves in the workspace (pointers into it).
+struct Prepared {
+    int64_t *first;                                      // [B + 1] first tile of each sequence
+    Start *start;                                        // [groups]
+    int *info;                                           // groups that have tiles, a sequence with the most cached tokens
+    int *depth;                                          // [B][N] ancestors
+    uint32_t *sees;                                      // [B][N][words] ancestors and self, a bit each (null: a chain)
+    uint8_t *odd;                                        // [B][H_kv][N] whether a node's values hold an infinity or NaN
+    void *k, *v;                                         // [B][H_kv][N][d] keys rotated, values without those
+};
+
 struct Work {
     AttendArgs a;
     Cut c;
+    Prepared p;
     float *part;                                         // [slots][RT/32][HD/32][16][64]
     float2 *ml;                                          // [slots][RT] running maximum (log2) and sum
+    int words;                                           // of a node's ancestors
+    int prep_blocks;                                     // of a sequence, in the first launch
 };
 
-// ---- the list of tiles -----------------------------------------------------------
 __device__ __forceinline__ int cached(const AttendArgs &a, int b) {
     const int64_t room = min((int64_t)a.max_pages << a.log2_page, (int64_t)1 << 30);
     return (int)min((int64_t)max(a.len[b], 0), room);
 }
-
-struct List {
-    int64_t total, shared;                               // tiles of all, of the shared keys
-    int groups;                                          // workgroups that have some
-    int longest;                                         // a sequence with the most cached tokens
-};
-
-template <int KT> __device__ __forceinline__ int64_t tiles_of(const Work &w, int len) {
-    const int own = max(len - w.a.shared, 0);
-    return (int64_t)w.a.H_kv * ((int64_t)w.c.units * ((own + KT - 1) / KT) + w.c.draft_tiles);
-}
-
-// One wave: the list's length, and how many tiles lie before sequence `until`.
-template <int KT> __device__ __forceinline__ List measure(const Work &w, int until, int64_t &before) {
-    const int lane = threadIdx.x & 63;
-    int64_t all = 0, part = 0;
-    int most = -1, who = 0;
-    for (int b = lane; b < w.a.B; b += 64) {
-        const int len = cached(w.a, b);
-        const int64_t t = tiles_of<KT>(w, len);
-        all += t;
-        part += b < until ? t : 0;
-        if (len > most) most = len, who = b;
-    }
-#pragma unroll
-    for (int d = 32; d > 0; d >>= 1) {
-        all += __shfl_xor(all, d);
-        part += __shfl_xor(part, d);
-        const int m = __shfl_xor(most, d), o = __shfl_xor(who, d);
-        if (m > most || (m == most && o < who)) most = m, who = o;
-    }
-    List l;
-    l.shared = (int64_t)w.a.H_kv * w.c.shared_units * w.c.shared_tiles;
-    l.total = l.shared + all;
-    l.groups = (int)min((int64_t)w.c.groups, l.total);
-    l.longest = who;
-    before = l.shared + part;
-    return l;
-}
-
-// One wave: the sequence that tile `at` (past the shared ones) belongs to, and its first tile.
-template <int KT> __device__ __forceinline__ int locate(const Work &w, const List &l, int64_t at, int64_t &first) {
-    const int lane = threadIdx.x & 63;
-    int64_t base = l.shared;
-    for (int b0 = 0; b0 < w.a.B; b0 += 64) {
-        const int64_t t = b0 + lane < w.a.B ? tiles_of<KT>(w, cached(w.a, b0 + lane)) : 0;
-        int64_t s = t;
-#pragma unroll
-        for (int d = 1; d < 64; d <<= 1) {
-            const int64_t y = __shfl_up(s, d);
-            if (lane >= d) s += y;
-        }
-        const uint64_t past = __ballot(base + s > at);
-        if (past) {
-            const int i = __builtin_ctzll(past);
-            first = base + __shfl(s - t, i);
-            return b0 + i;
-        }
-        base += __shfl(s, 63);
-    }
-    first = base;
-    return w.a.B;
-}
+__device__ __forceinline__ int own_tiles(const AttendArgs &a, int KT, int len) { return (max(len - a.shared, 0) + KT - 1) / KT; }
 
 // Workgroup whose part holds tile x, and the first tile of workgroup g.
 __device__ __forceinline__ int64_t first_of(int64_t total, int groups, int64_t g) { return total * g / groups; }
@@ -159,6 +123,190 @@ __device__ __forceinline__ int group_of(int64_t total, int groups, int64_t x) { 
 // and one that begins it and does not end it.
 __device__ __forceinline__ int64_t slot_of(int groups, int64_t unit, bool begins, bool ends, int g) {
     return begins && ends ? 2 * (int64_t)groups + unit : 2 * (int64_t)g + (begins ? 1 : 0);
+}
+
+// Position of a row's angles; past the rotation table its last.
+__device__ __forceinline__ int position(const AttendArgs &a, int len, int before, int b) {
+    const int p = len + before;
+    if (a.rot == 0 || p < a.positions) return p;
+    flag_error(a.err, b, TREEWY_FLAG_CACHE_FULL);
+    return a.positions - 1;
+}
+
+// ---- first launch --------------------------------------------------------------
+// Whether 16 bytes hold an infinity or NaN; and those as zeros.
+template <typename T> __device__ __forceinline__ bool not_finite(uint4 x) {
+    constexpr uint32_t E = 0x7f800000u;
+    bool odd = false;
+    const uint32_t w[4] = {x.x, x.y, x.z, x.w};
+#pragma unroll
+    for (int i = 0; i < 4; ++i) odd |= (w[i] & E) == E || (sizeof(T) == 2 && (w[i] << 16 & E) == E);
+    return odd;
+}
+template <typename T> __device__ __forceinline__ uint4 finite(uint4 x) {
+    float f[Granule<T>::N];
+    Granule<T>::wide(x, f);
+#pragma unroll
+    for (int i = 0; i < Granule<T>::N; ++i) f[i] = fabsf(f[i]) < INFINITY ? f[i] : 0.0f;
+    return Granule<T>::narrow(f);
+}
+
+// The list: first tiles, and where every group begins.  One workgroup.
+__device__ void make_list(const Work &w, int RT, int KT) {
+    __shared__ int64_t sums[THREADS];
+    __shared__ int most[THREADS], who[THREADS];
+    const AttendArgs &a = w.a;
+    const int tid = threadIdx.x, per = (a.B + THREADS - 1) / THREADS;
+    const int64_t shared = (int64_t)a.H_kv * w.c.shared_units * w.c.shared_tiles;
+    auto tiles_of = [&](int b) {
+        return (int64_t)a.H_kv * ((int64_t)w.c.units * own_tiles(a, KT, cached(a, b)) + w.c.draft_tiles);
+    };
+    int64_t sum = 0;
+    int top = -1, at = 0;
+    for (int b = tid * per; b < min(a.B, (tid + 1) * per); ++b) {
+        const int len = cached(a, b);
+        sum += tiles_of(b);
+        if (len > top) top = len, at = b;
+    }
+    sums[tid] = sum;
+    most[tid] = top;
+    who[tid] = at;
+    for (int d = 1; d < THREADS; d <<= 1) {
+        __syncthreads();
+        const int64_t x = tid >= d ? sums[tid - d] : 0;
+        const int m = tid >= d ? most[tid - d] : -1, o = tid >= d ? who[tid - d] : 0;
+        __syncthreads();
+        sums[tid] += x;
+        if (m >= most[tid]) most[tid] = m, who[tid] = o;
+    }
+    __syncthreads();
+    const int64_t total = shared + sums[THREADS - 1];
+    int64_t next = shared + sums[tid] - sum;
+    for (int b = tid * per; b < min(a.B, (tid + 1) * per); ++b) {
+        w.p.first[b] = next;
+        next += tiles_of(b);
+    }
+    if (tid == 0) w.p.first[a.B] = total;
+    const int groups = (int)min((int64_t)w.c.groups, total);
+    if (tid == 0) w.p.info[0] = groups, w.p.info[1] = who[THREADS - 1];
+    __threadfence_block();
+    __syncthreads();
+    for (int g = tid; g < groups; g += THREADS) {
+        const int64_t x = first_of(total, groups, g);
+        Start s{};
+        s.tiles = (int)(first_of(total, groups, g + 1) - x);
+        if (x < shared) {
+            const int n = (int)(x / w.c.shared_tiles);
+            s.b = -1;
+            s.h = n / w.c.shared_units;
+            s.rt = n - s.h * w.c.shared_units;
+            s.t0 = (int)(x - (int64_t)n * w.c.shared_tiles);
+        } else {
+            int lo = 0, hi = a.B;                        // first[lo] <= x < first[hi]
+            while (hi - lo > 1) {
+                const int mid = (lo + hi) / 2;
+                if (w.p.first[mid] <= x) lo = mid;
+                else hi = mid;
+            }
+            const int old = own_tiles(a, KT, cached(a, lo)), per_head = w.c.units * old + w.c.draft_tiles;
+            int left = (int)(x - w.p.first[lo]);
+            s.b = lo;
+            s.h = left / per_head;
+            left -= s.h * per_head;
+            for (s.rt = 0;; ++s.rt) {
+                const int tiles = old + draft_tiles_of(s.rt, RT, KT, w.c.G, a.N);
+                if (left < tiles) break;
+                left -= tiles;
+            }
+            s.t0 = left;
+        }
+        w.p.start[g] = s;
+    }
+}
+
+// Workgroups 0 .. B prep_blocks - 1 have the drafts, the last one the list.
+template <typename T, int HD> __global__ __launch_bounds__(THREADS) void prepare_kernel(Work w, int RT, int KT) {
+    constexpr int W = MAX_TREE / 32, E = Granule<T>::N, GRAN = HD / E;
+    __shared__ uint32_t sees[MAX_TREE][W];
+    __shared__ int up[MAX_TREE], depth[MAX_TREE];
+    const AttendArgs &a = w.a;
+    const int b = blockIdx.x / w.prep_blocks, chunk = blockIdx.x - b * w.prep_blocks, t = threadIdx.x;
+    if (b == a.B) {
+        make_list(w, RT, KT);
+        return;
+    }
+    const int len = cached(a, b);
+    if (chunk == 0 && t == 0 && a.len[b] != len) flag_error(a.err, b, TREEWY_FLAG_CACHE_FULL);
+    static_assert(MAX_TREE <= THREADS, "a thread per node");
+    if (a.parent) {                                      // ancestors by pointer jumping; a bad parent counts as -1
+        int next = -1;
+        if (t < a.N) {
+            const int p = a.parent[(int64_t)b * a.N + t];
+            if (p >= 0 && p < t) next = p;
+            else if (p != -1) flag_error(a.err, b, TREEWY_FLAG_BAD_PARENT);
+            for (int i = 0; i < w.words; ++i) sees[t][i] = i == t / 32 ? 1u << (t % 32) : 0u;
+            up[t] = next;
+        }
+        while (__syncthreads_or(next >= 0)) {
+            uint32_t add[W];
+#pragma unroll
+            for (int i = 0; i < W; ++i) add[i] = next >= 0 && i < w.words ? sees[next][i] : 0u;
+            if (next >= 0) next = up[next];
+            __syncthreads();
+            if (t < a.N) {
+#pragma unroll
+                for (int i = 0; i < W; ++i)
+                    if (i < w.words) sees[t][i] |= add[i];
+                up[t] = next;
+            }
+        }
+        if (t < a.N) {
+            int n = -1;
+            for (int i = 0; i < w.words; ++i) n += __popc(sees[t][i]);
+            depth[t] = n;
+            if (chunk == 0) {
+                w.p.depth[(int64_t)b * a.N + t] = n;
+                for (int i = 0; i < w.words; ++i) w.p.sees[((int64_t)b * a.N + t) * w.words + i] = sees[t][i];
+            }
+        }
+    } else if (t < a.N) {
+        depth[t] = t;
+        if (chunk == 0) w.p.depth[(int64_t)b * a.N + t] = t;
+    }
+    __syncthreads();
+
+    // The draft's keys, rotated to their positions, and values.  A node's infinities and NaNs must not reach the nodes that
+    // do not see it (zero times them is NaN): values go without them, and the kernel adds them where they are seen.
+    const int half = a.rot / (2 * E), lanes = GRAN / 2, all = a.H_kv * a.N * lanes;
+    const int step = (all + w.prep_blocks * THREADS - 1) / (w.prep_blocks * THREADS) * THREADS;    // (a row in one wave)
+    for (int i = chunk * step + t; i < min(all, (chunk + 1) * step); i += THREADS) {
+        const int p = i % lanes, row = i / lanes, h = row / a.N, n = row - h * a.N;
+        const uint4 *k = reinterpret_cast<const uint4 *>((const T *)a.k + b * a.ks.seq + h * a.ks.head + n * a.ks.token);
+        const uint4 *v = reinterpret_cast<const uint4 *>((const T *)a.v + b * a.vs.seq + h * a.vs.head + n * a.vs.token);
+        const int64_t to = (((int64_t)b * a.H_kv + h) * a.N + n) * GRAN;
+        const bool turns = p < half;
+        const int lo = turns ? p : half + p, hi = turns ? p + half : lo + (lanes - half);
+        uint4 x = k[lo], y = k[hi], v0 = v[lo], v1 = v[hi];
+        if (turns) {
+            Angles<T> angles;
+            angles.load(a.cos, a.sin, (int64_t)position(a, len, depth[n], b) * (a.rot / 2), p * E);
+            const uint4 first = rotated<T>(x, y, angles, false);
+            y = rotated<T>(y, x, angles, true);
+            x = first;
+        }
+        const bool odd = not_finite<T>(v0) || not_finite<T>(v1);
+        if (odd) {
+            v0 = finite<T>(v0);
+            v1 = finite<T>(v1);
+        }
+        const uint64_t in_row = __ballot(odd) >> (t & 63 & ~(lanes - 1)) & ((1ull << lanes) - 1ull);
+        if (p == 0) w.p.odd[((int64_t)b * a.H_kv + h) * a.N + n] = in_row != 0;
+        uint4 *ko = (uint4 *)w.p.k + to, *vo = (uint4 *)w.p.v + to;
+        ko[lo] = x;
+        ko[hi] = y;
+        vo[lo] = v0;
+        vo[hi] = v1;
+    }
 }
 
 // ---- results -----------------------------------------------------------------
@@ -178,365 +326,264 @@ template <typename T> __device__ __forceinline__ T *out_row(const AttendArgs &a,
 }
 
 __device__ __forceinline__ float other_half(float x) { return __shfl_xor(x, 32); }
+__device__ __forceinline__ int uniform(int x) { return __builtin_amdgcn_readfirstlane(x); }
 
 // ---- the kernel ----------------------------------------------------------------
-template <typename S> struct Lds {
-    typedef uint4 Tile[2 * S::TILE];                     // keys, then values
-    uint32_t sees[MAX_TREE][MAX_TREE / 32];              // ancestors and self, a bit each
-    int16_t up[MAX_TREE];                                // the next pointer jump's target
-    int16_t depth[MAX_TREE];                             // ancestors
-    uint32_t odd[MAX_TREE / 32];                         // nodes whose values hold an infinity or NaN, a bit each
-};
+// Waits for this wave's loads into LDS: vmcnt(0), the other counters as they are.  (By the builtin, which the compiler
+// understands: after it, reads of one tile do not wait for the loads of the next.)
+__device__ __forceinline__ void loads_done() { __builtin_amdgcn_s_waitcnt(0x0f70); }
 
-// Whether 16 bytes hold an infinity or NaN; and those as zeros.
-template <typename T> __device__ __forceinline__ bool not_finite(uint4 x) {
-    constexpr uint32_t E = 0x7f800000u;
-    bool odd = false;
-    const uint32_t w[4] = {x.x, x.y, x.z, x.w};
-#pragma unroll
-    for (int i = 0; i < 4; ++i) odd |= (w[i] & E) == E || (sizeof(T) == 2 && (w[i] << 16 & E) == E);
-    return odd;
-}
-template <typename T> __device__ __forceinline__ uint4 finite(uint4 x) {
-    float f[Granule<T>::N];
-    Granule<T>::wide(x, f);
-#pragma unroll
-    for (int i = 0; i < Granule<T>::N; ++i) f[i] = fabsf(f[i]) < INFINITY ? f[i] : 0.0f;
-    return Granule<T>::narrow(f);
-}
-
-// Ancestors of every node of sequence b by pointer jumping; a bad parent counts as -1.
-template <typename S> __device__ void climb(Lds<S> &s, const AttendArgs &a, int b) {
-    constexpr int W = MAX_TREE / 32, PER = (MAX_TREE + S::NT - 1) / S::NT;
-    const int words = (a.N + 31) / 32;
-    __syncthreads();
-    for (int t = threadIdx.x; t < a.N; t += S::NT) {
-        int p = a.parent[(int64_t)b * a.N + t];
-        if (p < -1 || p >= t) {
-            flag_error(a.err, b, TREEWY_FLAG_BAD_PARENT);
-            p = -1;
-        }
-        for (int i = 0; i < words; ++i) s.sees[t][i] = i == t / 32 ? 1u << (t % 32) : 0u;
-        s.up[t] = (int16_t)p;
-    }
-    for (bool more = true; more;) {
-        __syncthreads();
-        uint32_t add[PER][W];
-        int next[PER];
-        bool any = false;
-#pragma unroll
-        for (int k = 0; k < PER; ++k) {
-            const int t = threadIdx.x + k * S::NT;
-            next[k] = -1;
-            const int p = t < a.N ? s.up[t] : -1;
-#pragma unroll
-            for (int i = 0; i < W; ++i) add[k][i] = p >= 0 && i < words ? s.sees[p][i] : 0u;
-            if (p >= 0) next[k] = s.up[p];
-            any |= next[k] >= 0;
-        }
-        more = __syncthreads_or(any);
-#pragma unroll
-        for (int k = 0; k < PER; ++k) {
-            const int t = threadIdx.x + k * S::NT;
-            if (t < a.N) {
-#pragma unroll
-                for (int i = 0; i < W; ++i)
-                    if (i < words) s.sees[t][i] |= add[k][i];
-                s.up[t] = (int16_t)next[k];
-            }
-        }
-    }
-    __syncthreads();
-    for (int t = threadIdx.x; t < a.N; t += S::NT) {
-        int n = -1;
-        for (int i = 0; i < words; ++i) n += __popc(s.sees[t][i]);
-        s.depth[t] = (int16_t)n;
-    }
-    __syncthreads();
-}
-
-// A unit: a row tile with the tiles of its keys.
-struct Unit {
-    bool shared;
-    int b, h, rt;                                        // (b: whose page table is read)
-    int old_tiles, tiles;                                // tiles of cached keys, of all
-    int first_key, len;                                  // the cached keys [first_key, len)
-};
-
-// One lane's query row.
-struct Row {
-    bool live;
-    int b, n, head, pos, limit;                          // cached keys below `limit` are seen
-};
-
-template <typename S> struct Part {
-    const Work &w;
-    const AttendArgs &a;
-    Lds<S> &s;
-    const Unit &u;
-    const int lane, wave, hg, wr, wk;
-    Row row;
-    uint4 q[S::STEPS];
-    f32x16 acc[S::DT];
-    float m, l, c;
-
+template <typename S> __global__ __launch_bounds__(S::NT, S::HD <= 128 && sizeof(typename S::T) == 2 ? 2 : 1) void attend_kernel(Work w) {
     using T = typename S::T;
-    static constexpr int E = S::E, GRAN = S::GRAN, KT = S::KT;
+    constexpr int KT = S::KT, RT = S::RT, GRAN = S::GRAN, E = S::E, ROW = 16 * GRAN, WK = S::WK, WR = S::WR, DT = S::DT;
+    constexpr int NB = KT / (32 * WK);                   // blocks of 32 keys that a wave has of a tile
+    constexpr int PER_LOAD = 64 / GRAN;                  // rows of one load
+    constexpr bool BF = sizeof(T) == 2;
+    __shared__ uint4 tile0[2 * S::TILE], tile1[2 * S::TILE];
+    const AttendArgs &a = w.a;
+    const int lane = threadIdx.x & 63, wave = uniform(threadIdx.x >> 6), hg = lane >> 5, wr = wave / WK, wk = wave % WK;
+    // Consecutive parts of the list on one XCD (workgroups go to the eight in turn): row tiles that read the same keys meet in its L2.
+    const unsigned per = gridDim.x / 8;
+    int g = blockIdx.x;
+    if (blockIdx.x < per * 8) g = (int)((blockIdx.x & 7u) * per + (blockIdx.x >> 3));
 
-    __device__ __forceinline__ Part(const Work &w, Lds<S> &s, const Unit &u)
-        : w(w), a(w.a), s(s), u(u), lane(threadIdx.x & 63), wave(__builtin_amdgcn_readfirstlane(threadIdx.x >> 6)),
-          hg(lane >> 5), wr(wave / S::WK), wk(wave % S::WK) {}
-
-    __device__ __forceinline__ bool chain() const { return a.parent == nullptr; }
-    __device__ __forceinline__ int position(int len, int before, int b) const {
-        const int p = len + before;
-        if (a.rot && p >= a.positions) {
-            flag_error(a.err, b, TREEWY_FLAG_CACHE_FULL);
-            return a.positions - 1;
-        }
-        return p;
+    int b, h, rt, t0, left, longest = 0;
+    if (w.c.groups) {
+        const int groups = uniform(w.p.info[0]);
+        longest = uniform(w.p.info[1]);
+        if (groups < w.c.groups) g = blockIdx.x;         // (fewer tiles than workgroups: one each, on all XCDs)
+        if (g >= groups) return;
+        const Start s = w.p.start[g];
+        b = uniform(s.b), h = uniform(s.h), rt = uniform(s.rt), t0 = uniform(s.t0), left = uniform(s.tiles);
+    } else {                                             // one unit
+        b = g / (a.H_kv * w.c.units);
+        const int n = g - b * a.H_kv * w.c.units;
+        h = n / w.c.units;
+        rt = n - h * w.c.units;
+        t0 = 0;
+        left = INT32_MAX;
     }
 
-    __device__ __forceinline__ void begin() {
-        const int r = u.rt * S::RT + wr * 32 + (lane & 31);
-        const int64_t rows = u.shared ? (int64_t)a.B * w.c.M : w.c.M;
-        row.live = r < rows;
-        const int x = row.live ? r : 0;
-        row.b = u.shared ? x / w.c.M : u.b;
-        const int rr = u.shared ? x - row.b * w.c.M : x;
-        row.n = rr / w.c.G;
-        row.head = u.h * w.c.G + rr - row.n * w.c.G;
-        const int len = u.shared ? cached(a, row.b) : u.len;
-        row.limit = u.shared ? min(len, u.len) : u.len;
-        int before = row.n;
-        if (!chain()) {
-            if (!u.shared) before = s.depth[row.n];
-            else {                                       // (few nodes where keys are shared)
-                before = 0;
-                for (int t = row.n;;) {
-                    const int p = a.parent[(int64_t)row.b * a.N + t];
-                    if (p < 0 || p >= t) break;
-                    t = p;
-                    ++before;
+    // Addresses in a tile's LDS, the same for every tile: keys of the lane's row from its granule hg on (granule 2 i + hg is
+    // i << 5 away by exclusive or), values by the four keys that a lane reads at once (32 columns further: dt << 6, too).
+    const int row_at = (lane & 31) * ROW + place<GRAN>(lane & 31, hg) * 16;
+    int val_at[2] = {};
+    if constexpr (BF) {
+        const int j = (lane >> 2) & 3, y = lane & 3, c16 = (lane >> 4) & 1;
+#pragma unroll
+        for (int e = 0; e < 2; ++e) {
+            const int r = 8 * e + 4 * hg + j;
+            val_at[e] = r * ROW + place<GRAN>(r, c16 * 2 + (y >> 1)) * 16 + (y & 1) * 8;
+        }
+    } else {
+        val_at[0] = 4 * hg * ROW + place<GRAN>(4 * hg, (lane & 31) / 4) * 16 + (lane & 3) * 4;
+    }
+    const float c = fmaxf(fabsf(a.scale) * LOG2E, 1e-30f);            // (a zero scale must not meet a masked score's infinity)
+    const uint32_t flip = a.scale < 0.0f ? (BF ? 0x80008000u : 0x80000000u) : 0u;
+    const uint32_t page_rows = (1u << a.log2_page) - 1u;
+    const int64_t page_bytes = (int64_t)a.H_kv * ROW << a.log2_page;
+
+    while (true) {
+        // the unit: its cached keys [first_key, len) in old_tiles, then the draft's
+        const bool shared = b < 0;
+        const int own_b = shared ? longest : b;
+        const int len_b = uniform(cached(a, own_b));
+        const int first_key = shared ? 0 : min(a.shared, len_b), len = shared ? min(a.shared, len_b) : len_b;
+        const int old_tiles = shared ? w.c.shared_tiles : (len - first_key + KT - 1) / KT;
+        const int tiles = shared ? old_tiles : old_tiles + draft_tiles_of(rt, RT, KT, w.c.G, a.N);
+        const int t1 = left < tiles - t0 ? t0 + left : tiles;
+        const int32_t *table = a.table + (int64_t)own_b * a.max_pages;
+        const char *kp = (const char *)a.k_pages + ((int64_t)h * ROW << a.log2_page);
+        const char *vp = (const char *)a.v_pages + ((int64_t)h * ROW << a.log2_page);
+        const int64_t draft = ((int64_t)own_b * a.H_kv + h) * a.N * ROW;
+
+        // Lane p: the p-th page of tile t's tokens, -1 where there is none or an invalid one.
+        auto pages_of = [&](int t) {
+            const int key0 = first_key + t * KT, end = min(key0 + KT, len), page = (key0 >> a.log2_page) + lane;
+            int id = -1;
+            if (t < old_tiles && page <= (end - 1) >> a.log2_page) {
+                id = table[page];
+                if ((unsigned)id >= (unsigned)a.n_pages) {
+                    id = -1;
+                    for (int s = shared ? 0 : b; s < (shared ? a.B : b + 1); ++s)
+                        if (cached(a, s) > page << a.log2_page) flag_error(a.err, s, TREEWY_FLAG_BAD_PAGE);
                 }
             }
-        }
-        row.pos = position(len, before, row.b);
-        if (a.len[row.b] != len) flag_error(a.err, row.b, TREEWY_FLAG_CACHE_FULL);
-
-        // the row's granules 2 i + hg, rotated, in the scale's sign
-        const uint4 *src = reinterpret_cast<const uint4 *>((const T *)a.q + row.b * a.qs.seq + row.head * a.qs.head +
-                                                           row.n * a.qs.token);
-        const int half = a.rot / (2 * E);
-        const uint32_t flip = a.scale < 0.0f ? (sizeof(T) == 2 ? 0x80008000u : 0x80000000u) : 0u;
-#pragma unroll
-        for (int i = 0; i < S::STEPS; ++i) {
-            const int g = 2 * i + hg;
-            uint4 x = src[g];
-            if (g < 2 * half) {
-                const bool second = g >= half;
-                const int i0 = second ? g - half : g;
-                Angles<T> w;
-                w.load(a.cos, a.sin, (int64_t)row.pos * (a.rot / 2), i0 * E);
-                x = rotated<T>(x, src[second ? i0 : g + half], w, second);
-            }
-            q[i] = make_uint4(x.x ^ flip, x.y ^ flip, x.z ^ flip, x.w ^ flip);
-        }
-        c = fmaxf(fabsf(a.scale) * LOG2E, 1e-30f);       // (a zero scale must not meet a masked score's infinity)
-        m = -INFINITY;
-        l = 0.0f;
-#pragma unroll
-        for (int dt = 0; dt < S::DT; ++dt) acc[dt] = f32x16{};
-    }
-
-    // The page of lane p's tokens in tile t: the tile's p-th page, -1 where it has none or an invalid one.
-    __device__ __forceinline__ int page_of(int t) {
-        const int key0 = u.first_key + t * KT, end = min(key0 + KT, u.len);
-        const int page = (key0 >> a.log2_page) + lane;
-        int id = -1;
-        if (t < u.old_tiles && page <= (end - 1) >> a.log2_page) {
-            id = a.table[(int64_t)u.b * a.max_pages + page];
-            if (id < 0 || id >= a.n_pages) {
-                id = -1;
-                if (u.shared) {                          // (every sequence that has the page says so)
-                    for (int b = 0; b < a.B; ++b)
-                        if (cached(a, b) > page << a.log2_page) flag_error(a.err, b, TREEWY_FLAG_BAD_PAGE);
-                } else flag_error(a.err, u.b, TREEWY_FLAG_BAD_PAGE);
-            }
-        }
-        return id;
-    }
-
-    // Issues the loads of tile t, whose pages page_of gave, into `tile`.
-    __device__ __forceinline__ void fetch(uint4 *tile, int t, int pages) {
-        if (t < u.old_tiles) {
-            const int key0 = u.first_key + t * KT, base = key0 >> a.log2_page;
+            return id;
+        };
+        auto pages_in = [&](int t) {                     // how many that is
+            const int key0 = first_key + t * KT, end = min(key0 + KT, len);
+            return t < old_tiles && end > key0 ? ((end - 1) >> a.log2_page) - (key0 >> a.log2_page) + 1 : 0;
+        };
+        // Issues the loads of tile t into `tile`.
+        auto fetch = [&](uint4 *tile, int t, int pages) {
+            const bool old = t < old_tiles;
+            const int ln = opaque(lane);                 // (see compute)
+            const int key0 = old ? first_key + t * KT : (t - old_tiles) * KT, end = old ? len : a.N;
+            const bool whole = key0 + KT <= end && (!old || __ballot(lane < pages_in(t) && pages < 0) == 0);
 #pragma unroll
             for (int i = 0; i < S::LOADS / S::WAVES; ++i) {
-                const int load = i * S::WAVES + wave, at = load * 64 + lane;
-                const int r = at / GRAN, g = place<GRAN>(r, at % GRAN), key = key0 + r;
-                const int id = __shfl(pages, ((key >> a.log2_page) - base) & 63);
-                const bool have = key < u.len && id >= 0;
-                const int64_t off =
-                    ((((int64_t)id * a.H_kv + u.h) << a.log2_page) + (key & ((1 << a.log2_page) - 1))) * GRAN + g;
-                const uint4 *k = have ? (const uint4 *)a.k_pages + off : zero_row + g % 64;
-                const uint4 *v = have ? (const uint4 *)a.v_pages + off : zero_row + g % 64;
+                const int load = i * S::WAVES + wave, r0 = load * PER_LOAD, r = r0 + ln / GRAN;
+                const int off = (ln / GRAN) * ROW + place<GRAN>(r, ln % GRAN) * 16;
+                const int key = key0 + r0;               // (the rows of a load are in one page)
+                const char *k, *v;
+                bool none = false;
+                if (old) {
+                    const int id = __builtin_amdgcn_readlane(pages, (key >> a.log2_page) - (key0 >> a.log2_page));
+                    const int64_t at = max(id, 0) * page_bytes + (key & page_rows) * ROW;
+                    k = kp + at;
+                    v = vp + at;
+                    none = id < 0;
+                } else {
+                    k = (const char *)w.p.k + draft + (int64_t)key * ROW;
+                    v = (const char *)w.p.v + draft + (int64_t)key * ROW;
+                }
+                k += off;
+                v += off;
+                if (!whole && (none || key0 + r >= end)) k = v = (const char *)(zero_row + lane % GRAN);
                 __builtin_amdgcn_global_load_lds((global_void *)k, (lds_void *)(tile + load * 64), 16, 0, 0);
                 __builtin_amdgcn_global_load_lds((global_void *)v, (lds_void *)(tile + S::TILE + load * 64), 16, 0, 0);
             }
-            return;
-        }
-        // The draft's own: keys rotated to their positions.  A node's infinities and NaNs must not reach the nodes that do
-        // not see it (zero times them is NaN), so values go in without them and odd_values adds them where they are seen.
-        const int node0 = (t - u.old_tiles) * KT, half = a.rot / (2 * E);
-        for (int i = threadIdx.x; i < KT * GRAN / 2; i += S::NT) {
-            const int r = i / (GRAN / 2), p = i % (GRAN / 2), n = node0 + r;
-            const bool turns = p < half;
-            const int lo = turns ? p : half + p, hi = turns ? p + half : lo + (GRAN / 2 - half);
-            uint4 x = make_uint4(0, 0, 0, 0), y = x, v0 = x, v1 = x;
-            if (n < a.N) {
-                const uint4 *k = reinterpret_cast<const uint4 *>((const T *)a.k + u.b * a.ks.seq + u.h * a.ks.head + n * a.ks.token);
-                const uint4 *v = reinterpret_cast<const uint4 *>((const T *)a.v + u.b * a.vs.seq + u.h * a.vs.head + n * a.vs.token);
-                x = k[lo];
-                y = k[hi];
-                v0 = v[lo];
-                v1 = v[hi];
-                if (turns) {
-                    Angles<T> w;
-                    w.load(a.cos, a.sin, (int64_t)position(u.len, chain() ? n : s.depth[n], u.b) * (a.rot / 2), p * E);
-                    const uint4 first = rotated<T>(x, y, w, false);
-                    y = rotated<T>(y, x, w, true);
-                    x = first;
-                }
-                if (not_finite<T>(v0) || not_finite<T>(v1)) {
-                    atomicOr(&s.odd[n / 32], 1u << (n % 32));
-                    v0 = finite<T>(v0);
-                    v1 = finite<T>(v1);
+        };
+
+        __syncthreads();                                 // (the last part's LDS is read)
+        int pages = pages_of(t0), ahead = pages_of(t0 + 1);
+        fetch(tile0, t0, pages);
+
+        // the lane's query row
+        const int r = rt * RT + wr * 32 + (lane & 31);
+        const bool live = r < (shared ? a.B * w.c.M : w.c.M);
+        const int x0 = live ? r : 0, row_b = shared ? x0 / w.c.M : b, rr = shared ? x0 - row_b * w.c.M : x0;
+        const int node = rr / w.c.G, head = h * w.c.G + rr - node * w.c.G;
+        const int row_len = cached(a, row_b), limit = min(row_len, len);
+        uint4 q[S::STEPS], q_rest[S::LO > 0 ? S::LO : 1];
+        {
+            const uint4 *src = reinterpret_cast<const uint4 *>((const T *)a.q + row_b * a.qs.seq + head * a.qs.head + node * a.qs.token);
+            const int half = a.rot / (2 * E);
+            int64_t angle_row = 0;
+            if (a.rot) angle_row = (int64_t)position(a, row_len, w.p.depth[(int64_t)row_b * a.N + node], row_b) * (a.rot / 2);
+#pragma unroll
+            for (int i = 0; i < S::STEPS; ++i) {
+                const int gr = 2 * i + hg;
+                uint4 x = src[gr];
+                if (i < S::TURN && gr < 2 * half) {
+                    const bool second = gr >= half;
+                    const int i0 = second ? gr - half : gr;
+                    Angles<T> angles;
+                    angles.load(a.cos, a.sin, angle_row, i0 * E);
+                    if constexpr (BF) rotated_split(x, src[second ? i0 : gr + half], angles, second, x, q_rest[i < S::LO ? i : 0]);
+                    else x = rotated<T>(x, src[second ? i0 : gr + half], angles, second);
+                } else if (i < S::LO) q_rest[i < S::LO ? i : 0] = make_uint4(0, 0, 0, 0);
+                q[i] = make_uint4(x.x ^ flip, x.y ^ flip, x.z ^ flip, x.w ^ flip);
+                if (i < S::LO) {
+                    uint4 &y = q_rest[i < S::LO ? i : 0];
+                    y = make_uint4(y.x ^ flip, y.y ^ flip, y.z ^ flip, y.w ^ flip);
                 }
             }
-            tile[r * GRAN + place<GRAN>(r, lo)] = x;
-            tile[r * GRAN + place<GRAN>(r, hi)] = y;
-            tile[S::TILE + r * GRAN + place<GRAN>(r, lo)] = v0;
-            tile[S::TILE + r * GRAN + place<GRAN>(r, hi)] = v1;
         }
-    }
-
-    __device__ __forceinline__ bool sees(int node) const {
-        return chain() ? node <= row.n : (s.sees[row.n][node / 32] >> (node % 32)) & 1u;
-    }
-
-    // The infinities and NaNs that were left out of the draft's values, where they are seen.
-    __device__ void odd_values() {
-        for (int i = 0; i < (a.N + 31) / 32; ++i)
-            for (uint32_t bits = s.odd[i]; bits; bits &= bits - 1) {
-                const int n = 32 * i + __builtin_ctz(bits);
-                if (!sees(n)) continue;
-                const T *v = (const T *)a.v + u.b * a.vs.seq + u.h * a.vs.head + n * a.vs.token;
+        const bool some = __any(live);
+        float m = -INFINITY, l = 0.0f;
+        f32x16 acc[DT];
 #pragma unroll
-                for (int dt = 0; dt < S::DT; ++dt)
+        for (int dt = 0; dt < DT; ++dt) acc[dt] = f32x16{};
+
+        auto compute = [&](const uint4 *tile, int t, int now) {
+            const char *kt = reinterpret_cast<const char *>(tile) + wk * 32 * NB * ROW, *vt = kt + S::TILE * 16;
+            const bool old = t < old_tiles;
+            // (opaque: addresses are formed where they are used, not kept for all of the loop)
+            const int key_at = opaque(row_at), val0 = opaque(val_at[0]), val1 = BF ? opaque(val_at[BF]) : 0;
+            const int first = (old ? first_key + t * KT : (t - old_tiles) * KT) + wk * 32 * NB;
+            // Both products read their operands a group ahead of the group that they multiply; sched_barrier keeps it so (left
+            // alone the compiler reads each operand right before its use).
+            f32x16 x[NB];
 #pragma unroll
-                    for (int r = 0; r < 16; ++r) {
-                        const float x = to_f32(v[dt * 32 + acc_row(r, hg)]);
-                        if (!(fabsf(x) < INFINITY)) acc[dt][r] += x;
+            for (int n = 0; n < NB; ++n) x[n] = f32x16{};
+            constexpr int KG = S::STEPS / 2;             // groups of two steps
+            uint4 kf[2][2 * NB];
+            auto read_keys = [&](int group) {
+#pragma unroll
+                for (int j = 0; j < 2; ++j)
+#pragma unroll
+                    for (int n = 0; n < NB; ++n)
+                        kf[group & 1][j * NB + n] = *reinterpret_cast<const uint4 *>(kt + n * 32 * ROW + (key_at ^ ((2 * group + j) << 5)));
+            };
+            read_keys(0);
+#pragma unroll
+            for (int group = 0; group < KG; ++group) {
+                if (group + 1 < KG) read_keys(group + 1);
+                __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+                for (int j = 0; j < 2; ++j) {
+                    const int i = 2 * group + j;
+#pragma unroll
+                    for (int n = 0; n < NB; ++n) {
+                        const uint4 k = kf[group & 1][j * NB + n];
+                        if constexpr (BF) {
+                            x[n] = mma(__builtin_bit_cast(bf16x8, k), __builtin_bit_cast(bf16x8, q[i]), x[n]);
+                        } else {
+                            const f32x4 kv = __builtin_bit_cast(f32x4, k), qv = __builtin_bit_cast(f32x4, q[i]);
+#pragma unroll
+                            for (int e = 0; e < 4; ++e) x[n] = mma_f32(kv[e], qv[e], x[n]);
+                        }
                     }
-            }
-    }
-
-    // Scores of the block of 32 keys that begins at row k0 of `tile`.
-    __device__ __forceinline__ f32x16 scores(const uint4 *tile, int k0) {
-        f32x16 x{};
-        const int r = k0 + (lane & 31);
+                    if (i < S::LO)
 #pragma unroll
-        for (int i = 0; i < S::STEPS; ++i) {
-            const uint4 k = tile[r * GRAN + place<GRAN>(r, 2 * i + hg)];
-            if constexpr (sizeof(T) == 2) {
-                x = mma(__builtin_bit_cast(bf16x8, k), __builtin_bit_cast(bf16x8, q[i]), x);
-            } else {
-                const f32x4 kf = __builtin_bit_cast(f32x4, k), qf = __builtin_bit_cast(f32x4, q[i]);
-#pragma unroll
-                for (int e = 0; e < 4; ++e) x = mma_f32(kf[e], qf[e], x);
-            }
-        }
-        return x;
-    }
-
-    // Adds V^T P^T of the block.
-    __device__ __forceinline__ void add_values(const uint4 *tile, int k0, const f32x16 &p) {
-        const uint4 *v = tile + S::TILE;
-        if constexpr (sizeof(T) == 2) {
-            bf16x8 pb[2];
-#pragma unroll
-            for (int h = 0; h < 2; ++h) {
-                u32x4 x;
-#pragma unroll
-                for (int j = 0; j < 4; ++j) x[j] = pack_bf2(p[8 * h + 2 * j], p[8 * h + 2 * j + 1]);
-                pb[h] = __builtin_bit_cast(bf16x8, x);
-            }
-            const int j = (lane >> 2) & 3, y = lane & 3, c16 = (lane >> 4) & 1;
-#pragma unroll
-            for (int dt = 0; dt < S::DT; ++dt) {
-                const int g = dt * 4 + c16 * 2 + (y >> 1);
-#pragma unroll
-                for (int h = 0; h < 2; ++h) {
-                    s16x4 x[2];
-#pragma unroll
-                    for (int e = 0; e < 2; ++e) {
-                        const int r = k0 + 16 * h + 8 * e + 4 * hg + j;
-                        const char *at = reinterpret_cast<const char *>(v + r * GRAN + place<GRAN>(r, g)) + (y & 1) * 8;
-                        x[e] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4 *)at);
-                    }
-                    acc[dt] = mma(both8(__builtin_bit_cast(uint2, x[0]), __builtin_bit_cast(uint2, x[1])), pb[h], acc[dt]);
+                        for (int n = 0; n < NB; ++n)
+                            x[n] = mma(__builtin_bit_cast(bf16x8, kf[group & 1][j * NB + n]),
+                                       __builtin_bit_cast(bf16x8, q_rest[i < S::LO ? i : 0]), x[n]);
                 }
+                __builtin_amdgcn_sched_barrier(0);
             }
-        } else {
+            constexpr int VG = BF ? NB * DT : 1;         // groups of two products of 16 keys with 32 values
+            s16x4 vf[2][4];
+            auto read_values = [&](int group) {
 #pragma unroll
-            for (int dt = 0; dt < S::DT; ++dt)
+                for (int j = 0; j < 2; ++j) {
+                    const int s = (2 * group + j) / DT, dt = (2 * group + j) % DT;
 #pragma unroll
-                for (int r = 0; r < 16; ++r) {
-                    const int key = k0 + acc_row(r, hg), d = dt * 32 + (lane & 31);
-                    const float x = reinterpret_cast<const float *>(v + key * GRAN + place<GRAN>(key, d / 4))[d % 4];
-                    acc[dt] = mma_f32(x, p[r], acc[dt]);
+                    for (int e = 0; e < 2; ++e)
+                        vf[group & 1][2 * j + e] =
+                            __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4 *)(vt + s * 16 * ROW + ((e ? val1 : val0) ^ (dt << 6))));
                 }
-        }
-    }
-
-    __device__ __forceinline__ void compute(const uint4 *tile, int t, int pages) {
-        const bool old = t < u.old_tiles;
-        const int key0 = old ? u.first_key + t * KT : (t - u.old_tiles) * KT;
-        if (!__any(row.live)) return;
-        uint64_t bad = 0;
-        if (old) {
-            const int n_pages = ((min(key0 + KT, u.len) - 1) >> a.log2_page) - (key0 >> a.log2_page) + 1;
-            bad = __ballot(lane < n_pages && pages < 0);
-        }
-#pragma unroll 1
-        for (int kb = wk; kb < KT / 32; kb += S::WK) {
-            const int first = key0 + kb * 32;
-            if (old ? first >= u.len : first >= a.N) break;
-            f32x16 x = scores(tile, kb * 32);
+            };
+            if constexpr (BF) read_values(0);
             if (old) {
-                if (__any(first + 32 > row.limit)) {
-                    const int rel = row.limit - first;
+                if (__any(first + 32 * NB > limit)) {
 #pragma unroll
-                    for (int r = 0; r < 16; ++r) x[r] = acc_row(r, hg) < rel ? x[r] : -INFINITY;
+                    for (int n = 0; n < NB; ++n)
+#pragma unroll
+                        for (int r = 0; r < 16; ++r) x[n][r] = acc_row(r, hg) < limit - first - 32 * n ? x[n][r] : -INFINITY;
                 }
+                const uint64_t bad = __ballot(lane < pages_in(t) && now < 0);
                 if (bad) {
+                    const int base = (first_key + t * KT) >> a.log2_page;
 #pragma unroll
-                    for (int r = 0; r < 16; ++r) {
-                        const int page = ((first + acc_row(r, hg)) >> a.log2_page) - (key0 >> a.log2_page);
-                        x[r] = (bad >> (page & 63)) & 1 ? -INFINITY : x[r];
-                    }
+                    for (int n = 0; n < NB; ++n)
+#pragma unroll
+                        for (int r = 0; r < 16; ++r) {
+                            const int page = ((first + 32 * n + acc_row(r, hg)) >> a.log2_page) - base;
+                            x[n][r] = (bad >> (page & 63)) & 1 ? -INFINITY : x[n][r];
+                        }
                 }
             } else {
-                const int ahead = row.n - first;
-                uint32_t sees = chain() ? (ahead >= 31 ? ~0u : ahead < 0 ? 0u : (2u << ahead) - 1u) : s.sees[row.n][first / 32];
-                sees >>= 4 * hg;
 #pragma unroll
-                for (int r = 0; r < 16; ++r) x[r] = (sees >> acc_row(r, 0)) & 1u ? x[r] : -INFINITY;
+                for (int n = 0; n < NB; ++n) {
+                    const int key = first + 32 * n, back = node - key;
+                    uint32_t sees = 0;
+                    if (key < a.N) {
+                        if (a.parent) sees = w.p.sees[((int64_t)b * a.N + node) * w.words + key / 32];
+                        else sees = back >= 31 ? ~0u : back < 0 ? 0u : (2u << back) - 1u;
+                    }
+                    sees >>= 4 * hg;
+#pragma unroll
+                    for (int r = 0; r < 16; ++r) x[n][r] = (sees >> acc_row(r, 0)) & 1u ? x[n][r] : -INFINITY;
+                }
             }
-            float top = x[0];
+            float top = x[0][0];
 #pragma unroll
-            for (int r = 1; r < 16; ++r) top = fmaxf(top, x[r]);
+            for (int n = 0; n < NB; ++n)
+#pragma unroll
+                for (int r = 0; r < 16; ++r) top = fmaxf(top, x[n][r]);
             top = fmaxf(top, other_half(top));
             // Sums are held relative to a maximum that may lag behind by a factor of 2^8: rescaling is rare then.
             if (__any((top - m) * c > 8.0f)) {
@@ -545,195 +592,150 @@ template <typename S> struct Part {
                 m = to;
                 l *= by;
 #pragma unroll
-                for (int dt = 0; dt < S::DT; ++dt) acc[dt] *= by;
+                for (int dt = 0; dt < DT; ++dt) acc[dt] *= by;
             }
             const float at = m == -INFINITY ? 0.0f : m * c;
 #pragma unroll
-            for (int r = 0; r < 16; ++r) {
-                x[r] = __builtin_amdgcn_exp2f(__builtin_fmaf(x[r], c, -at));
-                l += x[r];
+            for (int n = 0; n < NB; ++n)
+#pragma unroll
+                for (int r = 0; r < 16; ++r) {
+                    x[n][r] = __builtin_amdgcn_exp2f(__builtin_fmaf(x[n][r], c, -at));
+                    l += x[n][r];
+                }
+            if constexpr (BF) {
+                bf16x8 p[2 * NB];
+#pragma unroll
+                for (int s = 0; s < 2 * NB; ++s) {
+                    u32x4 pk;
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) pk[j] = pack_bf2(x[s / 2][8 * (s & 1) + 2 * j], x[s / 2][8 * (s & 1) + 2 * j + 1]);
+                    p[s] = __builtin_bit_cast(bf16x8, pk);
+                }
+#pragma unroll
+                for (int group = 0; group < VG; ++group) {
+                    if (group + 1 < VG) read_values(group + 1);
+                    __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+                    for (int j = 0; j < 2; ++j) {
+                        const int s = (2 * group + j) / DT, dt = (2 * group + j) % DT;
+                        acc[dt] = mma(both8(__builtin_bit_cast(uint2, vf[group & 1][2 * j]), __builtin_bit_cast(uint2, vf[group & 1][2 * j + 1])),
+                                      p[s], acc[dt]);
+                    }
+                    __builtin_amdgcn_sched_barrier(0);
+                }
+            } else {
+#pragma unroll
+                for (int n = 0; n < NB; ++n)
+#pragma unroll
+                    for (int dt = 0; dt < DT; ++dt)
+#pragma unroll
+                        for (int r = 0; r < 16; ++r) {   // (key acc_row(r, hg): place() moves by what r alone decides)
+                            const int move = (place<GRAN>(acc_row(r, 0), 0) * 16) ^ (dt << 7);
+                            const float y = *reinterpret_cast<const float *>(vt + (32 * n + acc_row(r, 0)) * ROW + (val0 ^ move));
+                            acc[dt] = mma_f32(y, x[n][r], acc[dt]);
+                        }
             }
-            add_values(tile, kb * 32, x);
+        };
+        auto step = [&](const uint4 *here, uint4 *next, int t) {
+            loads_done();
+            __syncthreads();
+            const int now = pages;
+            pages = ahead;
+            if (t + 1 < t1) {
+                fetch(next, t + 1, pages);
+                ahead = pages_of(t + 2);
+            }
+            if (some) compute(here, t, now);
+        };
+        for (int t = t0; t < t1; t += 2) {
+            step(tile0, tile1, t);
+            if (t + 1 < t1) step(tile1, tile0, t + 1);
         }
-    }
 
-    // Joins the key groups of each row group in its first wave.
-    __device__ __forceinline__ void join(float *lds) {
+        // the infinities and NaNs that were left out of the draft's values, where they are seen
+        if (!shared && t1 == tiles && wk == 0) {
+            const uint8_t *odd = w.p.odd + ((int64_t)b * a.H_kv + h) * a.N;
+            for (int i = 0; i < a.N; i += 64) {
+                uint64_t bits = __ballot(i + lane < a.N && odd[i + lane]);
+                for (; bits; bits &= bits - 1) {
+                    const int n = i + __builtin_ctzll(bits);
+                    const bool sees =
+                        a.parent ? (w.p.sees[((int64_t)b * a.N + node) * w.words + n / 32] >> (n % 32)) & 1u : n <= node;
+                    const T *v = (const T *)a.v + b * a.vs.seq + h * a.vs.head + n * a.vs.token;
+#pragma unroll
+                    for (int dt = 0; dt < DT; ++dt)
+#pragma unroll
+                        for (int r = 0; r < 16; ++r) {
+                            const float x = to_f32(v[dt * 32 + acc_row(r, hg)]);
+                            if (sees && !(fabsf(x) < INFINITY)) acc[dt][r] += x;
+                        }
+                }
+            }
+        }
+
+        // the key groups of each row group meet in its first wave
         l += other_half(l);
-        if constexpr (S::WK > 1) {
-            constexpr int WAVE = S::DT * 16 * 64;
+        if constexpr (WK > 1) {
+            constexpr int WAVE = DT * 16 * 64;
+            float *lds = reinterpret_cast<float *>(tile0);
+            float2 *stats = reinterpret_cast<float2 *>(tile1);
             __syncthreads();
             if (wk > 0) {
-                float *to = lds + ((wk - 1) * S::WR + wr) * WAVE;
+                float *to = lds + ((wk - 1) * WR + wr) * WAVE;
 #pragma unroll
-                for (int dt = 0; dt < S::DT; ++dt)
+                for (int dt = 0; dt < DT; ++dt)
 #pragma unroll
                     for (int r = 0; r < 16; ++r) to[(dt * 16 + r) * 64 + lane] = acc[dt][r];
-                float2 *st = reinterpret_cast<float2 *>(s.sees);                       // (the masks are done with)
-                st[wave * 64 + lane] = make_float2(m, l);
+                stats[wave * 64 + lane] = make_float2(m, l);
             }
             __syncthreads();
             if (wk == 0) {
-#pragma unroll
-                for (int k = 1; k < S::WK; ++k) {
-                    const float2 o = reinterpret_cast<const float2 *>(s.sees)[(wave + k) * 64 + lane];
+#pragma unroll 1
+                for (int k = 1; k < WK; ++k) {
+                    const float2 o = stats[(wave + k) * 64 + lane];
                     const float to = fmaxf(m, o.x);
                     const float by = m == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f((m - to) * c);
                     const float oby = o.x == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f((o.x - to) * c);
-                    const float *from = lds + ((k - 1) * S::WR + wr) * WAVE;
+                    const float *from = lds + ((k - 1) * WR + wr) * WAVE;
                     m = to;
                     l = l * by + o.y * oby;
 #pragma unroll
-                    for (int dt = 0; dt < S::DT; ++dt)
+                    for (int dt = 0; dt < DT; ++dt)
 #pragma unroll
                         for (int r = 0; r < 16; ++r) acc[dt][r] = acc[dt][r] * by + from[(dt * 16 + r) * 64 + lane] * oby;
                 }
             }
         }
-    }
-
-    __device__ __forceinline__ void finish() {           // a whole unit without shared keys
-        if (wk != 0 || !row.live) return;
-        T *o = out_row<T>(a, row.b, row.head, row.n);
-        const float by = 1.0f / l;
+        const bool begins = t0 == 0, ends = t1 == tiles;
+        if (wk == 0 && some) {
+            if (begins && ends && w.c.shared_tiles == 0) {
+                if (live) {
+                    T *o = out_row<T>(a, row_b, head, node);
+                    const float by = 1.0f / l;
 #pragma unroll
-        for (int dt = 0; dt < S::DT; ++dt) store_row<T>(o, dt, hg, acc[dt], by);
-    }
-
-    __device__ __forceinline__ void leave(int64_t slot) {
-        if (wk != 0 || !__any(row.live)) return;
-        float *to = w.part + (slot * S::WR + wr) * (32 * S::HD);
-#pragma unroll
-        for (int dt = 0; dt < S::DT; ++dt)
-#pragma unroll
-            for (int r = 0; r < 16; ++r) to[(dt * 16 + r) * 64 + lane] = acc[dt][r];
-        if (hg == 0) w.ml[slot * S::RT + wr * 32 + lane] = make_float2(m == -INFINITY ? -INFINITY : m * c, l);
-    }
-};
-
-// Waits for this wave's loads into LDS.
-__device__ __forceinline__ void loads_done() { asm volatile("s_waitcnt vmcnt(0)" ::: "memory"); }
-
-template <typename S> __global__ __launch_bounds__(S::NT) void attend_kernel(Work w) {
-    constexpr int KT = S::KT, RT = S::RT;
-    __shared__ typename Lds<S>::Tile tile0, tile1;
-    __shared__ Lds<S> s;
-    const AttendArgs &a = w.a;
-    // Consecutive parts of the list on one XCD (workgroups go to the eight in turn): row tiles that read the same keys meet in its L2.
-    const unsigned blocks = gridDim.x, per = blocks / 8;
-    int g = blockIdx.x, groups = 0;
-    if (blockIdx.x < per * 8) g = (int)((blockIdx.x & 7u) * per + (blockIdx.x >> 3));
-
-    int64_t at, end, first;                              // this group's tiles, and the current sequence's first
-    int b = -1, longest = 0;
-    if (w.c.groups) {
-        int64_t unused;
-        const List list = measure<KT>(w, 0, unused);
-        groups = list.groups;
-        if (groups < w.c.groups) g = blockIdx.x;         // (fewer tiles than workgroups: one each, on all XCDs)
-        if (g >= groups) return;
-        at = first_of(list.total, groups, g);
-        end = first_of(list.total, groups, g + 1);
-        longest = list.longest;
-        if (at >= list.shared) b = locate<KT>(w, list, at, first);
-        else first = list.shared;
-        at = __builtin_amdgcn_readfirstlane((int)(at >> 32)) * ((int64_t)1 << 32) + (uint32_t)__builtin_amdgcn_readfirstlane((int)at);
-        end = __builtin_amdgcn_readfirstlane((int)(end >> 32)) * ((int64_t)1 << 32) + (uint32_t)__builtin_amdgcn_readfirstlane((int)end);
-        first = __builtin_amdgcn_readfirstlane((int)(first >> 32)) * ((int64_t)1 << 32) +
-                (uint32_t)__builtin_amdgcn_readfirstlane((int)first);
-        b = __builtin_amdgcn_readfirstlane(b);
-    } else {                                             // one unit: its place in the list does not matter
-        b = g / (a.H_kv * w.c.units);
-        at = first = 0;
-        end = 1;
-    }
-    int climbed = -1;
-    const int64_t shared_all = (int64_t)a.H_kv * w.c.shared_units * w.c.shared_tiles;
-    while (at < end) {
-        // the unit that tile `at` belongs to, and its tiles [begin, begin + tiles) in the list
-        Unit u;
-        int64_t begin, id;
-        u.shared = b < 0;
-        if (u.shared) {
-            const int n = (int)(at / w.c.shared_tiles);
-            id = n;
-            u.h = n / w.c.shared_units;
-            u.rt = n - u.h * w.c.shared_units;
-            u.b = longest;
-            u.first_key = 0;
-            u.len = min(a.shared, cached(a, u.b));
-            u.old_tiles = u.tiles = w.c.shared_tiles;
-            begin = (int64_t)n * w.c.shared_tiles;
-        } else {
-            const int len = cached(a, b);
-            u.b = b;
-            u.len = len;
-            u.first_key = min(a.shared, len);
-            u.old_tiles = (len - u.first_key + KT - 1) / KT;
-            const int per_head = w.c.units * u.old_tiles + w.c.draft_tiles;
-            if (w.c.groups) {
-                int left = (int)(at - first);
-                u.h = left / per_head;
-                left -= u.h * per_head;
-                for (u.rt = 0;; ++u.rt) {
-                    u.tiles = u.old_tiles + draft_tiles_of(u.rt, RT, KT, w.c.G, a.N);
-                    if (left < u.tiles) break;
-                    left -= u.tiles;
+                    for (int dt = 0; dt < DT; ++dt) store_row<T>(o, dt, hg, acc[dt], by);
                 }
-                begin = at - left;
             } else {
-                const int n = g - b * a.H_kv * w.c.units;
-                u.h = n / w.c.units;
-                u.rt = n - u.h * w.c.units;
-                u.tiles = u.old_tiles + draft_tiles_of(u.rt, RT, KT, w.c.G, a.N);
-                begin = 0;
-                end = u.tiles;
+                const int64_t unit = shared ? (int64_t)h * w.c.shared_units + rt
+                                            : (int64_t)a.H_kv * w.c.shared_units + ((int64_t)b * a.H_kv + h) * w.c.units + rt;
+                const int64_t slot = slot_of(w.c.groups, unit, begins, ends, g);
+                float *to = w.part + (slot * WR + wr) * (32 * S::HD);
+#pragma unroll
+                for (int dt = 0; dt < DT; ++dt)
+#pragma unroll
+                    for (int r = 0; r < 16; ++r) to[(dt * 16 + r) * 64 + lane] = acc[dt][r];
+                if (hg == 0) w.ml[slot * RT + wr * 32 + lane] = make_float2(m == -INFINITY ? -INFINITY : m * c, l);
             }
-            id = (int64_t)a.H_kv * w.c.shared_units + ((int64_t)b * a.H_kv + u.h) * w.c.units + u.rt;
         }
-        const int t0 = (int)(at - begin), t1 = (int)min((int64_t)u.tiles, end - begin);
-        if (!u.shared && a.parent && climbed != b) {
-            climb<S>(s, a, b);
-            climbed = b;
-        }
-        {
-            Part<S> p(w, s, u);
-            __syncthreads();                             // (the last part's LDS is read)
-            if (threadIdx.x < MAX_TREE / 32) s.odd[threadIdx.x] = 0;
-            __syncthreads();
-            int pages = p.page_of(t0), ahead = p.page_of(t0 + 1);
-            p.fetch(tile0, t0, pages);
-            p.begin();
-            auto step = [&](uint4 *here, uint4 *next, int t) {
-                loads_done();
-                __syncthreads();
-                const int now = pages;
-                pages = ahead;
-                if (t + 1 < t1) {
-                    p.fetch(next, t + 1, pages);
-                    ahead = p.page_of(t + 2);
-                }
-                p.compute(here, t, now);
-            };
-            for (int t = t0; t < t1; t += 2) {
-                step(tile0, tile1, t);
-                if (t + 1 < t1) step(tile1, tile0, t + 1);
-            }
-            if (!u.shared && p.wk == 0) p.odd_values();
-            p.join(reinterpret_cast<float *>(tile0));
-            if constexpr (S::WK > 1) climbed = -1;       // (join wrote over the masks)
-            const bool whole = t0 == 0 && t1 == u.tiles;
-            if (whole && w.c.shared_tiles == 0) p.finish();
-            else p.leave(slot_of(w.c.groups, id, t0 == 0, t1 == u.tiles, g));
-        }
-        at = begin + t1;
-        if (!w.c.groups) break;
-        if (u.shared) {
-            if (at >= shared_all) b = 0, first = at;
-        } else if (u.h == a.H_kv - 1 && u.rt == w.c.units - 1 && t1 == u.tiles) {
-            ++b;
-            first = at;
-        }
+
+        left -= t1 - t0;
+        if (left <= 0 || !w.c.groups) return;
+        t0 = 0;                                          // the next unit: row tiles, then heads, then sequences
+        if (++rt < (shared ? w.c.shared_units : w.c.units)) continue;
+        rt = 0;
+        if (++h < a.H_kv) continue;
+        h = 0;
+        ++b;
     }
 }
 
@@ -748,10 +750,9 @@ template <typename S> __global__ __launch_bounds__(256) void join_kernel(Work w)
     const int b = unit / (a.H_kv * w.c.units), n = unit - b * a.H_kv * w.c.units, h = n / w.c.units, rt = n - h * w.c.units;
     const int r = rt * RT + wr * 32 + (lane & 31);
     if (rt * RT + wr * 32 >= w.c.M) return;
-    int64_t before;
-    const List list = measure<KT>(w, b, before);
-    const int len = cached(a, b), old = (max(len - a.shared, 0) + KT - 1) / KT;
-    int64_t begin = before + (int64_t)h * (w.c.units * old + w.c.draft_tiles);
+    const int64_t total = w.p.first[a.B];
+    const int groups = w.p.info[0], old = own_tiles(a, KT, cached(a, b));
+    int64_t begin = w.p.first[b] + (int64_t)h * (w.c.units * old + w.c.draft_tiles);
     for (int i = 0; i < rt; ++i) begin += old + draft_tiles_of(i, RT, KT, w.c.G, a.N);
     const int64_t end = begin + old + draft_tiles_of(rt, RT, KT, w.c.G, a.N);
     const int64_t shared_ids = (int64_t)a.H_kv * w.c.shared_units;
@@ -761,8 +762,8 @@ template <typename S> __global__ __launch_bounds__(256) void join_kernel(Work w)
         int first, count, lane;
         int64_t unit;
     } span[2];
-    span[0].first = group_of(list.total, list.groups, begin);
-    span[0].count = group_of(list.total, list.groups, end - 1) - span[0].first + 1;
+    span[0].first = group_of(total, groups, begin);
+    span[0].count = group_of(total, groups, end - 1) - span[0].first + 1;
     span[0].unit = shared_ids + unit;
     span[0].lane = wr * 32 + (lane & 31);
     span[1].count = 0;
@@ -771,14 +772,12 @@ template <typename S> __global__ __launch_bounds__(256) void join_kernel(Work w)
     if (w.c.shared_tiles && live) {
         const int64_t row = (int64_t)b * w.c.M + r;
         const int64_t id = (int64_t)h * w.c.shared_units + row / RT;
-        span[1].first = group_of(list.total, list.groups, id * w.c.shared_tiles);
-        span[1].count = group_of(list.total, list.groups, (id + 1) * w.c.shared_tiles - 1) - span[1].first + 1;
+        span[1].first = group_of(total, groups, id * w.c.shared_tiles);
+        span[1].count = group_of(total, groups, (id + 1) * w.c.shared_tiles - 1) - span[1].first + 1;
         span[1].unit = id;
         span[1].lane = (int)(row % RT);
     }
-    auto slot = [&](const Span &x, int i) {
-        return slot_of(w.c.groups, x.unit, i == 0, i == x.count - 1, x.first + i);
-    };
+    auto slot = [&](const Span &x, int i) { return slot_of(w.c.groups, x.unit, i == 0, i == x.count - 1, x.first + i); };
     float top = -INFINITY;
     if (live)
         for (int k = 0; k < 2; ++k)
@@ -826,24 +825,54 @@ template <typename S> Cut cut(int shared, int N, int B, int H_q, int H_kv) {
         c.shared_units = (int)(((int64_t)B * c.M + S::RT - 1) / S::RT);
         c.shared_tiles = (shared + S::KT - 1) / S::KT;
     }
-    const int resident = compute_units() * (2 * (int)sizeof(typename Lds<S>::Tile) > 65536 + 16384 ? 1 : 2);
+    const int resident = compute_units() * (4 * S::TILE * 16 > 80 * 1024 ? 1 : 2);
     if (shared == 0 && all >= 3 * (int64_t)resident) return c;        // enough units to even themselves out
     c.groups = resident;
     c.slots = 2 * (int64_t)resident + (shared > 0 ? (int64_t)H_kv * c.shared_units + all : 0);
     return c;
 }
 
-template <typename S> size_t bytes(const Cut &c) {
-    return (size_t)c.slots * S::RT * (S::HD * sizeof(float) + sizeof(float2));
+// The workspace's parts; bytes of all.
+template <typename S> size_t lay_out(Work &w, void *workspace) {
+    const AttendArgs &a = w.a;
+    size_t at = 0;
+    auto take = [&](auto *&p, size_t n) {
+        p = reinterpret_cast<std::remove_reference_t<decltype(p)>>((char *)workspace + at);
+        at += (n * sizeof(*p) + 255) / 256 * 256;
+    };
+    w.words = (a.N + 31) / 32;
+    char *k, *v;
+    const size_t rows = (size_t)a.B * a.H_kv * a.N;
+    take(w.p.first, a.B + 1);
+    take(w.p.info, 2);
+    take(w.p.start, w.c.groups);
+    take(w.p.odd, rows);
+    take(w.p.depth, (size_t)a.B * a.N);
+    take(w.p.sees, (size_t)a.B * a.N * w.words);
+    take(k, rows * S::HD * sizeof(typename S::T));
+    take(v, rows * S::HD * sizeof(typename S::T));
+    w.p.k = k, w.p.v = v;
+    take(w.part, (size_t)w.c.slots * S::RT * S::HD);
+    take(w.ml, (size_t)w.c.slots * S::RT);
+    return at;
+}
+
+template <typename S> size_t bytes(int shared, int N, int B, int H_q, int H_kv) {
+    Work w{};
+    w.a.N = N, w.a.B = B, w.a.H_kv = H_kv;
+    w.c = cut<S>(shared, N, B, H_q, H_kv);
+    return lay_out<S>(w, nullptr);
 }
 
 template <typename S> hipError_t run(const AttendArgs &a, void *workspace, hipStream_t stream) {
-    Work w;
+    Work w{};
     w.a = a;
     w.c = cut<S>(a.shared, a.N, a.B, a.H_q, a.H_kv);
-    w.part = (float *)workspace;
-    w.ml = (float2 *)(w.part + w.c.slots * S::RT * S::HD);
-    const int64_t units = (int64_t)a.B * a.H_kv * w.c.units;
+    lay_out<S>(w, workspace);
+    const int64_t units = (int64_t)a.B * a.H_kv * w.c.units, pairs = (int64_t)a.H_kv * a.N * (S::GRAN / 2);
+    w.prep_blocks = (int)((pairs + 4 * THREADS - 1) / (4 * THREADS));
+    hipLaunchKernelGGL((prepare_kernel<typename S::T, S::HD>), dim3((unsigned)(a.B * w.prep_blocks + 1)), dim3(THREADS), 0, stream, w,
+                       S::RT, S::KT);
     hipLaunchKernelGGL((attend_kernel<S>), dim3((unsigned)(w.c.groups ? w.c.groups : units)), dim3(S::NT), 0, stream, w);
     if (w.c.groups)
         hipLaunchKernelGGL((join_kernel<S>), dim3((unsigned)(units * S::WR * S::DT)), dim3(256), 0, stream, w);
@@ -851,27 +880,34 @@ template <typename S> hipError_t run(const AttendArgs &a, void *workspace, hipSt
 }
 
 // The kernel of a call: f(Shape) for its type, head and rows.  Few rows leave the keys to the waves; tiles of 64 KiB keep
-// enough loads in flight where HBM bounds the call.
-template <typename F> auto choose(int rows, int d, bool f32, F &&f) {
+// enough loads in flight where HBM bounds the call.  TURN: steps of a row that may rotate.
+template <typename F> auto choose(int rows, int d, int rot, bool f32, F &&f) {
     if (f32) {
-        if (d == 64) return rows <= 32 ? f(Shape<float, 64, 1, 4, 128>{}) : f(Shape<float, 64, 4, 1, 128>{});
-        if (d == 128) return rows <= 32 ? f(Shape<float, 128, 1, 2, 64>{}) : f(Shape<float, 128, 4, 1, 64>{});
-        return rows <= 32 ? f(Shape<float, 256, 1, 1, 32>{}) : f(Shape<float, 256, 4, 1, 32>{});
+        if (d == 64) return rows <= 32 ? f(Shape<float, 64, 1, 4, 128, 8>{}) : f(Shape<float, 64, 4, 1, 128, 8>{});
+        if (d == 128) return rows <= 32 ? f(Shape<float, 128, 1, 2, 64, 16>{}) : f(Shape<float, 128, 4, 1, 64, 16>{});
+        return rows <= 32 ? f(Shape<float, 256, 1, 1, 32, 32>{}) : f(Shape<float, 256, 4, 1, 32, 32>{});
     }
     if (d == 64) {
-        if (rows <= 32) return f(Shape<__bf16, 64, 1, 4, 128>{});
-        return rows <= 64 ? f(Shape<__bf16, 64, 2, 2, 128>{}) : f(Shape<__bf16, 64, 4, 1, 128>{});
+        if (rows <= 32) return f(Shape<__bf16, 64, 1, 4, 128, 4>{});
+        return rows <= 64 ? f(Shape<__bf16, 64, 2, 2, 128, 4>{}) : f(Shape<__bf16, 64, 4, 1, 128, 4>{});
     }
     if (d == 128) {
-        if (rows <= 32) return f(Shape<__bf16, 128, 1, 4, 128>{});
-        return rows <= 64 ? f(Shape<__bf16, 128, 2, 2, 128>{}) : f(Shape<__bf16, 128, 4, 1, 64>{});
+        if (rows <= 32) return f(Shape<__bf16, 128, 1, 4, 128, 8>{});
+        return rows <= 64 ? f(Shape<__bf16, 128, 2, 2, 128, 8>{}) : f(Shape<__bf16, 128, 4, 1, 64, 8>{});
     }
-    if (rows <= 32) return f(Shape<__bf16, 256, 1, 2, 64>{});
-    return rows <= 64 ? f(Shape<__bf16, 256, 2, 2, 64>{}) : f(Shape<__bf16, 256, 4, 1, 64>{});
+    if (rot <= 64) {
+        if (rows <= 32) return f(Shape<__bf16, 256, 1, 2, 64, 4>{});
+        return rows <= 64 ? f(Shape<__bf16, 256, 2, 2, 64, 4>{}) : f(Shape<__bf16, 256, 4, 1, 64, 4>{});
+    }
+    if (rows <= 32) return f(Shape<__bf16, 256, 1, 2, 64, 16>{});
+    return rows <= 64 ? f(Shape<__bf16, 256, 2, 2, 64, 16>{}) : f(Shape<__bf16, 256, 4, 1, 64, 16>{});
 }
 
 // Shared keys are read once for all where few rows of each sequence would read them: past that they are not what bounds.
-int shared_used(int shared, int N, int B, int H_q, int H_kv) { return B > 1 && N * (H_q / H_kv) <= 64 && N <= 16 ? shared : 0; }
+// Whole tiles only; what is left of the last belongs to each sequence.
+int shared_used(int shared, int N, int B, int H_q, int H_kv) {
+    return B > 1 && N * (H_q / H_kv) <= 64 && N <= 16 ? shared / 128 * 128 : 0;
+}
 
 int rows_of(int shared, int N, int B, int H_q, int H_kv) { return N * (H_q / H_kv) * (shared > 0 ? B : 1); }
 
@@ -879,15 +915,13 @@ int rows_of(int shared, int N, int B, int H_q, int H_kv) { return N * (H_q / H_k
 
 size_t tree_attention_workspace(int shared, int N, int B, int H_q, int H_kv, int d, bool f32) {
     shared = shared_used(shared, N, B, H_q, H_kv);
-    return choose(rows_of(shared, N, B, H_q, H_kv), d, f32, [&](auto s) {
-        using S = decltype(s);
-        return bytes<S>(cut<S>(shared, N, B, H_q, H_kv));
-    });
+    return choose(rows_of(shared, N, B, H_q, H_kv), d, 0, f32, [&](auto s) { return bytes<decltype(s)>(shared, N, B, H_q, H_kv); });
 }
 
 hipError_t launch_tree_attention(AttendArgs a, int d, bool f32, void *workspace, hipStream_t stream) {
     a.shared = shared_used(a.shared, a.N, a.B, a.H_q, a.H_kv);
-    return choose(rows_of(a.shared, a.N, a.B, a.H_q, a.H_kv), d, f32, [&](auto s) { return run<decltype(s)>(a, workspace, stream); });
+    return choose(rows_of(a.shared, a.N, a.B, a.H_q, a.H_kv), d, a.rot, f32,
+                  [&](auto s) { return run<decltype(s)>(a, workspace, stream); });
 }
 
 }  // namespace treewy

@@ -60,4 +60,17 @@ template <typename T> __device__ __forceinline__ uint4 rotated(uint4 x, uint4 y,
     return Granule<T>::narrow(f);
 }
 
+// The same of bf16 granules as two bf16, x ~= hi + rest (16 bits).
+__device__ __forceinline__ void rotated_split(uint4 x, uint4 y, const Angles<__bf16> &a, bool second, uint4 &hi, uint4 &rest) {
+    float f[8], g[8];
+    Granule<__bf16>::wide(x, f);
+    Granule<__bf16>::wide(y, g);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) f[i] = f[i] * a.c[i] + (second ? g[i] : -g[i]) * a.s[i];
+    bf16x8 h, r;
+    split8(f, h, r);
+    hi = __builtin_bit_cast(uint4, h);
+    rest = __builtin_bit_cast(uint4, r);
+}
+
 }  // namespace treewy
