@@ -39,6 +39,8 @@ typedef __attribute__((address_space(3))) void lds_void;
 
 __device__ __attribute__((aligned(16))) const uint4 zero_row[64] = {};   // what masked rows load
 
+__device__ __forceinline__ uint4 operator^(uint4 x, uint32_t y) { return make_uint4(x.x ^ y, x.y ^ y, x.z ^ y, x.w ^ y); }
+
 __device__ __forceinline__ f32x16 mma_f32(float a, float b, f32x16 c) {
     return __builtin_amdgcn_mfma_f32_32x32x2f32(a, b, c, 0, 0, 0);
 }
@@ -54,6 +56,8 @@ template <typename T_, int HD_, int WR_, int WK_, int KT_, int TURN_> struct Sha
     static constexpr int TURN = TURN_, LO = sizeof(T) == 2 ? TURN : 0;
     static constexpr int TILE = KT * GRAN;               // granules of a tile's keys (and of its values)
     static constexpr int LOADS = TILE / 64;              // wave-wide loads of them
+    static constexpr bool Q_FIRST = RT * (GRAN + (LO > 0 ? 2 * TURN : 0)) > 2 * TILE;    // queries need both tiles' LDS on their way
+    static_assert(RT * GRAN <= 2 * TILE && RT * 2 * TURN <= 2 * TILE, "queries fit there");
     static_assert(KT % (32 * WK) == 0 && LOADS % WAVES == 0, "every wave has as much");
     static_assert((WK - 1) * WR * 32 * HD * 4 <= 2 * TILE * 16, "key groups meet in one tile's LDS");
     static_assert(128 % KT == 0, "shared keys end with a tile");
@@ -103,13 +107,14 @@ struct Work {
     AttendArgs a;
     Cut c;
     Prepared p;
-    float *part;                                         // [slots][RT/32][HD/32][16][64]
+    float *part;                                         // [slots][RT/32][HD/32][4][64][4]
     float2 *ml;                                          // [slots][RT] running maximum (log2) and sum
     int words;                                           // of a node's ancestors
     int prep_blocks;                                     // of a sequence, in the first launch
 };
 
-__device__ __forceinline__ int cached(const AttendArgs &a, int b) {
+// (A: AttendArgs, or the same in the kernel's argument segment)
+template <typename A> __device__ __forceinline__ int cached(const A &a, int b) {
     const int64_t room = min((int64_t)a.max_pages << a.log2_page, (int64_t)1 << 30);
     return (int)min((int64_t)max(a.len[b], 0), room);
 }
@@ -126,7 +131,7 @@ __device__ __forceinline__ int64_t slot_of(int groups, int64_t unit, bool begins
 }
 
 // Position of a row's angles; past the rotation table its last.
-__device__ __forceinline__ int position(const AttendArgs &a, int len, int before, int b) {
+template <typename A> __device__ __forceinline__ int position(const A &a, int len, int before, int b) {
     const int p = len + before;
     if (a.rot == 0 || p < a.positions) return p;
     flag_error(a.err, b, TREEWY_FLAG_CACHE_FULL);
@@ -321,45 +326,64 @@ template <typename T> __device__ __forceinline__ void store_row(T *o, int dt, in
     }
 }
 
-template <typename T> __device__ __forceinline__ T *out_row(const AttendArgs &a, int b, int head, int n) {
+template <typename T, typename A> __device__ __forceinline__ T *out_row(const A &a, int b, int head, int n) {
     return (T *)a.o + b * a.os.seq + head * a.os.head + n * a.os.token;
 }
 
 __device__ __forceinline__ float other_half(float x) { return __shfl_xor(x, 32); }
 __device__ __forceinline__ int uniform(int x) { return __builtin_amdgcn_readfirstlane(x); }
 
+// A wave's O^T: [HD/32][4][64 lanes][4], the four values of a row that follow one another side by side.
+template <int DT> __device__ __forceinline__ void put(float *to, int lane, const f32x16 (&x)[DT]) {
+#pragma unroll
+    for (int dt = 0; dt < DT; ++dt)
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+            *reinterpret_cast<f32x4 *>(to + ((dt * 4 + j) * 64 + lane) * 4) =
+                f32x4{x[dt][4 * j], x[dt][4 * j + 1], x[dt][4 * j + 2], x[dt][4 * j + 3]};
+}
+
 // ---- the kernel ----------------------------------------------------------------
+// The kernel's arguments where they lie, read anew after each call of this: kept in scalar registers over the main loop they
+// were more than there are, and were spilled to the lanes of vector registers.
+typedef const __attribute__((address_space(4))) Work Args;
+__device__ __forceinline__ Args *arguments() {
+    Args *w = (Args *)__builtin_amdgcn_kernarg_segment_ptr();
+    asm volatile("" : "+s"(w));
+    return w;
+}
+
 // Waits for this wave's loads into LDS: vmcnt(0), the other counters as they are.  (By the builtin, which the compiler
 // understands: after it, reads of one tile do not wait for the loads of the next.)
 __device__ __forceinline__ void loads_done() { __builtin_amdgcn_s_waitcnt(0x0f70); }
 
-template <typename S> __global__ __launch_bounds__(S::NT, S::HD <= 128 && sizeof(typename S::T) == 2 ? 2 : 1) void attend_kernel(Work w) {
+template <typename S> __global__ __launch_bounds__(S::NT, S::HD <= 128 && sizeof(typename S::T) == 2 ? 2 : 1) void attend_kernel(Work) {
     using T = typename S::T;
     constexpr int KT = S::KT, RT = S::RT, GRAN = S::GRAN, E = S::E, ROW = 16 * GRAN, WK = S::WK, WR = S::WR, DT = S::DT;
     constexpr int NB = KT / (32 * WK);                   // blocks of 32 keys that a wave has of a tile
     constexpr int PER_LOAD = 64 / GRAN;                  // rows of one load
     constexpr bool BF = sizeof(T) == 2;
     __shared__ uint4 tile0[2 * S::TILE], tile1[2 * S::TILE];
-    const AttendArgs &a = w.a;
     const int lane = threadIdx.x & 63, wave = uniform(threadIdx.x >> 6), hg = lane >> 5, wr = wave / WK, wk = wave % WK;
+    Args *w = arguments();
     // Consecutive parts of the list on one XCD (workgroups go to the eight in turn): row tiles that read the same keys meet in its L2.
     const unsigned per = gridDim.x / 8;
     int g = blockIdx.x;
     if (blockIdx.x < per * 8) g = (int)((blockIdx.x & 7u) * per + (blockIdx.x >> 3));
 
     int b, h, rt, t0, left, longest = 0;
-    if (w.c.groups) {
-        const int groups = uniform(w.p.info[0]);
-        longest = uniform(w.p.info[1]);
-        if (groups < w.c.groups) g = blockIdx.x;         // (fewer tiles than workgroups: one each, on all XCDs)
+    if (w->c.groups) {
+        const int groups = uniform(w->p.info[0]);
+        longest = uniform(w->p.info[1]);
+        if (groups < w->c.groups) g = blockIdx.x;        // (fewer tiles than workgroups: one each, on all XCDs)
         if (g >= groups) return;
-        const Start s = w.p.start[g];
+        const Start s = w->p.start[g];
         b = uniform(s.b), h = uniform(s.h), rt = uniform(s.rt), t0 = uniform(s.t0), left = uniform(s.tiles);
     } else {                                             // one unit
-        b = g / (a.H_kv * w.c.units);
-        const int n = g - b * a.H_kv * w.c.units;
-        h = n / w.c.units;
-        rt = n - h * w.c.units;
+        b = g / (w->a.H_kv * w->c.units);
+        const int n = g - b * w->a.H_kv * w->c.units;
+        h = n / w->c.units;
+        rt = n - h * w->c.units;
         t0 = 0;
         left = INT32_MAX;
     }
@@ -378,65 +402,69 @@ template <typename S> __global__ __launch_bounds__(S::NT, S::HD <= 128 && sizeof
     } else {
         val_at[0] = 4 * hg * ROW + place<GRAN>(4 * hg, (lane & 31) / 4) * 16 + (lane & 3) * 4;
     }
-    const float c = fmaxf(fabsf(a.scale) * LOG2E, 1e-30f);            // (a zero scale must not meet a masked score's infinity)
-    const uint32_t flip = a.scale < 0.0f ? (BF ? 0x80008000u : 0x80000000u) : 0u;
-    const uint32_t page_rows = (1u << a.log2_page) - 1u;
-    const int64_t page_bytes = (int64_t)a.H_kv * ROW << a.log2_page;
-
     while (true) {
+        w = arguments();
+        const auto &a = w->a;
+        const int log2_page = a.log2_page, n_pages = a.n_pages, N = a.N;
+        const float c = fmaxf(fabsf(a.scale) * LOG2E, 1e-30f);        // (a zero scale must not meet a masked score's infinity)
+        const uint32_t page_rows = (1u << log2_page) - 1u;
+        const int64_t page_bytes = (int64_t)a.H_kv * ROW << log2_page;
         // the unit: its cached keys [first_key, len) in old_tiles, then the draft's
         const bool shared = b < 0;
         const int own_b = shared ? longest : b;
         const int len_b = uniform(cached(a, own_b));
         const int first_key = shared ? 0 : min(a.shared, len_b), len = shared ? min(a.shared, len_b) : len_b;
-        const int old_tiles = shared ? w.c.shared_tiles : (len - first_key + KT - 1) / KT;
-        const int tiles = shared ? old_tiles : old_tiles + draft_tiles_of(rt, RT, KT, w.c.G, a.N);
+        const int old_tiles = shared ? w->c.shared_tiles : (len - first_key + KT - 1) / KT;
+        const int tiles = shared ? old_tiles : old_tiles + draft_tiles_of(rt, RT, KT, w->c.G, N);
         const int t1 = left < tiles - t0 ? t0 + left : tiles;
         const int32_t *table = a.table + (int64_t)own_b * a.max_pages;
-        const char *kp = (const char *)a.k_pages + ((int64_t)h * ROW << a.log2_page);
-        const char *vp = (const char *)a.v_pages + ((int64_t)h * ROW << a.log2_page);
-        const int64_t draft = ((int64_t)own_b * a.H_kv + h) * a.N * ROW;
+        const char *kp = (const char *)a.k_pages + ((int64_t)h * ROW << log2_page);
+        const char *vp = (const char *)a.v_pages + ((int64_t)h * ROW << log2_page);
+        const int64_t draft = ((int64_t)own_b * a.H_kv + h) * N * ROW;
+        const char *dk = (const char *)w->p.k + draft, *dv = (const char *)w->p.v + draft;
+        const uint32_t *tree = a.parent ? w->p.sees : nullptr;
+        const int words = w->words;
 
         // Lane p: the p-th page of tile t's tokens, -1 where there is none or an invalid one.
         auto pages_of = [&](int t) {
-            const int key0 = first_key + t * KT, end = min(key0 + KT, len), page = (key0 >> a.log2_page) + lane;
+            const int key0 = first_key + t * KT, end = min(key0 + KT, len), page = (key0 >> log2_page) + lane;
             int id = -1;
-            if (t < old_tiles && page <= (end - 1) >> a.log2_page) {
+            if (t < old_tiles && page <= (end - 1) >> log2_page) {
                 id = table[page];
-                if ((unsigned)id >= (unsigned)a.n_pages) {
+                if ((unsigned)id >= (unsigned)n_pages) {
                     id = -1;
-                    for (int s = shared ? 0 : b; s < (shared ? a.B : b + 1); ++s)
-                        if (cached(a, s) > page << a.log2_page) flag_error(a.err, s, TREEWY_FLAG_BAD_PAGE);
+                    Args *w = arguments();
+                    for (int s = shared ? 0 : b; s < (shared ? w->a.B : b + 1); ++s)
+                        if (cached(w->a, s) > page << log2_page) flag_error(w->a.err, s, TREEWY_FLAG_BAD_PAGE);
                 }
             }
             return id;
         };
         auto pages_in = [&](int t) {                     // how many that is
             const int key0 = first_key + t * KT, end = min(key0 + KT, len);
-            return t < old_tiles && end > key0 ? ((end - 1) >> a.log2_page) - (key0 >> a.log2_page) + 1 : 0;
+            return t < old_tiles && end > key0 ? ((end - 1) >> log2_page) - (key0 >> log2_page) + 1 : 0;
         };
         // Issues the loads of tile t into `tile`.
         auto fetch = [&](uint4 *tile, int t, int pages) {
             const bool old = t < old_tiles;
-            const int ln = opaque(lane);                 // (see compute)
-            const int key0 = old ? first_key + t * KT : (t - old_tiles) * KT, end = old ? len : a.N;
+            const int key0 = old ? first_key + t * KT : (t - old_tiles) * KT, end = old ? len : N;
             const bool whole = key0 + KT <= end && (!old || __ballot(lane < pages_in(t) && pages < 0) == 0);
-#pragma unroll
-            for (int i = 0; i < S::LOADS / S::WAVES; ++i) {
-                const int load = i * S::WAVES + wave, r0 = load * PER_LOAD, r = r0 + ln / GRAN;
-                const int off = (ln / GRAN) * ROW + place<GRAN>(r, ln % GRAN) * 16;
+#pragma unroll 1
+            for (int load = wave; load < S::LOADS; load += S::WAVES) {
+                const int r0 = load * PER_LOAD, r = r0 + lane / GRAN;
+                const int off = (lane / GRAN) * ROW + place<GRAN>(r, lane % GRAN) * 16;
                 const int key = key0 + r0;               // (the rows of a load are in one page)
                 const char *k, *v;
                 bool none = false;
                 if (old) {
-                    const int id = __builtin_amdgcn_readlane(pages, (key >> a.log2_page) - (key0 >> a.log2_page));
+                    const int id = __builtin_amdgcn_readlane(pages, (key >> log2_page) - (key0 >> log2_page));
                     const int64_t at = max(id, 0) * page_bytes + (key & page_rows) * ROW;
                     k = kp + at;
                     v = vp + at;
                     none = id < 0;
                 } else {
-                    k = (const char *)w.p.k + draft + (int64_t)key * ROW;
-                    v = (const char *)w.p.v + draft + (int64_t)key * ROW;
+                    k = dk + key * ROW;
+                    v = dv + key * ROW;
                 }
                 k += off;
                 v += off;
@@ -448,38 +476,66 @@ template <typename S> __global__ __launch_bounds__(S::NT, S::HD <= 128 && sizeof
 
         __syncthreads();                                 // (the last part's LDS is read)
         int pages = pages_of(t0), ahead = pages_of(t0 + 1);
-        fetch(tile0, t0, pages);
+        if constexpr (!S::Q_FIRST) fetch(tile0, t0, pages);
 
         // the lane's query row
         const int r = rt * RT + wr * 32 + (lane & 31);
-        const bool live = r < (shared ? a.B * w.c.M : w.c.M);
-        const int x0 = live ? r : 0, row_b = shared ? x0 / w.c.M : b, rr = shared ? x0 - row_b * w.c.M : x0;
-        const int node = rr / w.c.G, head = h * w.c.G + rr - node * w.c.G;
+        const bool live = r < (shared ? a.B * w->c.M : w->c.M);
+        const int x0 = live ? r : 0, row_b = shared ? x0 / w->c.M : b, rr = shared ? x0 - row_b * w->c.M : x0;
+        const int node = rr / w->c.G, head = h * w->c.G + rr - node * w->c.G;
         const int row_len = cached(a, row_b), limit = min(row_len, len);
+        // Queries go through LDS: a row's granules are read side by side, and the rotation is one short loop (unrolled over a
+        // lane's own granules it was a third of the kernel's instructions, each run once and most of them not in the
+        // instruction cache).
         uint4 q[S::STEPS], q_rest[S::LO > 0 ? S::LO : 1];
         {
-            const uint4 *src = reinterpret_cast<const uint4 *>((const T *)a.q + row_b * a.qs.seq + head * a.qs.head + node * a.qs.token);
+            constexpr int HALF = GRAN / 2, ROWS = 64 / HALF, TG = 2 * S::TURN;
+            uint4 *hi = tile1 + wr * 32 * GRAN, *rest = (S::Q_FIRST ? tile0 : tile1 + RT * GRAN) + wr * 32 * TG;
+            const int64_t src = row_b * a.qs.seq + head * a.qs.head + node * a.qs.token;
             const int half = a.rot / (2 * E);
-            int64_t angle_row = 0;
-            if (a.rot) angle_row = (int64_t)position(a, row_len, w.p.depth[(int64_t)row_b * a.N + node], row_b) * (a.rot / 2);
-#pragma unroll
-            for (int i = 0; i < S::STEPS; ++i) {
-                const int gr = 2 * i + hg;
-                uint4 x = src[gr];
-                if (i < S::TURN && gr < 2 * half) {
-                    const bool second = gr >= half;
-                    const int i0 = second ? gr - half : gr;
+            const int at = a.rot ? position(a, row_len, w->p.depth[(int64_t)row_b * N + node], row_b) : 0;
+            const uint32_t flip = a.scale < 0.0f ? (BF ? 0x80008000u : 0x80000000u) : 0u;
+#pragma unroll 1
+            for (int r0 = wk * ROWS; r0 < 32; r0 += WK * ROWS) {
+                const int r = r0 + lane / HALF, p = lane % HALF;
+                const bool turns = p < half;
+                const int lo = turns ? p : half + p, up = turns ? p + half : lo + (HALF - half);
+                const uint4 *x = reinterpret_cast<const uint4 *>((const T *)a.q + __shfl(src, r));
+                const int pos = __shfl(at, r);           // (here, where every lane takes part)
+                uint4 x0 = x[lo], x1 = x[up];
+                if (turns) {
                     Angles<T> angles;
-                    angles.load(a.cos, a.sin, angle_row, i0 * E);
-                    if constexpr (BF) rotated_split(x, src[second ? i0 : gr + half], angles, second, x, q_rest[i < S::LO ? i : 0]);
-                    else x = rotated<T>(x, src[second ? i0 : gr + half], angles, second);
-                } else if (i < S::LO) q_rest[i < S::LO ? i : 0] = make_uint4(0, 0, 0, 0);
-                q[i] = make_uint4(x.x ^ flip, x.y ^ flip, x.z ^ flip, x.w ^ flip);
-                if (i < S::LO) {
-                    uint4 &y = q_rest[i < S::LO ? i : 0];
-                    y = make_uint4(y.x ^ flip, y.y ^ flip, y.z ^ flip, y.w ^ flip);
+                    angles.load(a.cos, a.sin, (int64_t)pos * (a.rot / 2), p * E);
+                    if constexpr (BF) {
+                        uint4 y0, y1, z0, z1;
+                        rotated_split(x0, x1, angles, false, y0, z0);
+                        rotated_split(x1, x0, angles, true, y1, z1);
+                        x0 = y0;
+                        x1 = y1;
+                        if (lo < TG) rest[r * TG + place<TG>(r, lo)] = z0 ^ flip;
+                        if (up < TG) rest[r * TG + place<TG>(r, up)] = z1 ^ flip;
+                    } else {
+                        const uint4 first = rotated<T>(x0, x1, angles, false);
+                        x1 = rotated<T>(x1, x0, angles, true);
+                        x0 = first;
+                    }
+                } else if constexpr (BF) {
+                    if (lo < TG) rest[r * TG + place<TG>(r, lo)] = make_uint4(0, 0, 0, 0);
+                    if (up < TG) rest[r * TG + place<TG>(r, up)] = make_uint4(0, 0, 0, 0);
                 }
+                hi[r * GRAN + place<GRAN>(r, lo)] = x0 ^ flip;
+                hi[r * GRAN + place<GRAN>(r, up)] = x1 ^ flip;
             }
+            __syncthreads();
+            const int r = lane & 31;
+#pragma unroll
+            for (int i = 0; i < S::STEPS; ++i) q[i] = hi[r * GRAN + place<GRAN>(r, 2 * i + hg)];
+#pragma unroll
+            for (int i = 0; i < S::LO; ++i) q_rest[i] = rest[r * TG + place<TG>(r, 2 * i + hg)];
+        }
+        if constexpr (S::Q_FIRST) {
+            __syncthreads();
+            fetch(tile0, t0, pages);
         }
         const bool some = __any(live);
         float m = -INFINITY, l = 0.0f;
@@ -547,33 +603,20 @@ template <typename S> __global__ __launch_bounds__(S::NT, S::HD <= 128 && sizeof
                 }
             };
             if constexpr (BF) read_values(0);
-            if (old) {
-                if (__any(first + 32 * NB > limit)) {
-#pragma unroll
-                    for (int n = 0; n < NB; ++n)
-#pragma unroll
-                        for (int r = 0; r < 16; ++r) x[n][r] = acc_row(r, hg) < limit - first - 32 * n ? x[n][r] : -INFINITY;
-                }
-                const uint64_t bad = __ballot(lane < pages_in(t) && now < 0);
-                if (bad) {
-                    const int base = (first_key + t * KT) >> a.log2_page;
-#pragma unroll
-                    for (int n = 0; n < NB; ++n)
-#pragma unroll
-                        for (int r = 0; r < 16; ++r) {
-                            const int page = ((first + 32 * n + acc_row(r, hg)) >> a.log2_page) - base;
-                            x[n][r] = (bad >> (page & 63)) & 1 ? -INFINITY : x[n][r];
-                        }
-                }
-            } else {
+            // What the row does not see: keys past its limit or of invalid pages, nodes that are not its ancestors.
+            const uint64_t bad = old ? __ballot(lane < pages_in(t) && now < 0) : 0;
+            if (!old || bad || __any(first + 32 * NB > limit)) {
 #pragma unroll
                 for (int n = 0; n < NB; ++n) {
-                    const int key = first + 32 * n, back = node - key;
-                    uint32_t sees = 0;
-                    if (key < a.N) {
-                        if (a.parent) sees = w.p.sees[((int64_t)b * a.N + node) * w.words + key / 32];
-                        else sees = back >= 31 ? ~0u : back < 0 ? 0u : (2u << back) - 1u;
-                    }
+                    const int key = first + 32 * n, have = old ? limit - key : node + 1 - key;
+                    uint32_t sees = have >= 32 ? ~0u : have <= 0 ? 0u : (1u << have) - 1u;
+                    if (!old && tree) sees = key < N ? tree[((int64_t)b * N + node) * words + key / 32] : 0u;
+                    if (bad)
+#pragma unroll 1
+                        for (int i = 0; i < 32; ++i) {
+                            const int page = ((key + i) >> log2_page) - ((first_key + t * KT) >> log2_page);
+                            if ((bad >> (page & 63)) & 1u) sees &= ~(1u << i);
+                        }
                     sees >>= 4 * hg;
 #pragma unroll
                     for (int r = 0; r < 16; ++r) x[n][r] = (sees >> acc_row(r, 0)) & 1u ? x[n][r] : -INFINITY;
@@ -653,24 +696,28 @@ template <typename S> __global__ __launch_bounds__(S::NT, S::HD <= 128 && sizeof
         }
 
         // the infinities and NaNs that were left out of the draft's values, where they are seen
+        w = arguments();
         if (!shared && t1 == tiles && wk == 0) {
-            const uint8_t *odd = w.p.odd + ((int64_t)b * a.H_kv + h) * a.N;
-            for (int i = 0; i < a.N; i += 64) {
-                uint64_t bits = __ballot(i + lane < a.N && odd[i + lane]);
-                for (; bits; bits &= bits - 1) {
-                    const int n = i + __builtin_ctzll(bits);
-                    const bool sees =
-                        a.parent ? (w.p.sees[((int64_t)b * a.N + node) * w.words + n / 32] >> (n % 32)) & 1u : n <= node;
-                    const T *v = (const T *)a.v + b * a.vs.seq + h * a.vs.head + n * a.vs.token;
+            const auto &a = w->a;
+            const uint8_t *odd = w->p.odd + ((int64_t)b * a.H_kv + h) * N;
+            uint64_t any = 0;
+            for (int i = 0; i < N; i += 64) any |= __ballot(i + lane < N && odd[i + lane]);
+            if (any)
 #pragma unroll
-                    for (int dt = 0; dt < DT; ++dt)
+                for (int dt = 0; dt < DT; ++dt)
 #pragma unroll
-                        for (int r = 0; r < 16; ++r) {
-                            const float x = to_f32(v[dt * 32 + acc_row(r, hg)]);
-                            if (sees && !(fabsf(x) < INFINITY)) acc[dt][r] += x;
+                    for (int j = 0; j < 4; ++j)
+#pragma unroll 1
+                        for (int n = 0; n < N; ++n) {
+                            const bool seen = a.parent ? (w->p.sees[((int64_t)b * N + node) * words + n / 32] >> (n % 32)) & 1u : n <= node;
+                            if (!odd[n] || !seen) continue;
+                            const T *v = (const T *)a.v + b * a.vs.seq + h * a.vs.head + n * a.vs.token + dt * 32 + 8 * j + 4 * hg;
+#pragma unroll
+                            for (int r = 0; r < 4; ++r) {
+                                const float y = to_f32(v[r]);
+                                if (!(fabsf(y) < INFINITY)) acc[dt][4 * j + r] += y;
+                            }
                         }
-                }
-            }
         }
 
         // the key groups of each row group meet in its first wave
@@ -681,11 +728,7 @@ template <typename S> __global__ __launch_bounds__(S::NT, S::HD <= 128 && sizeof
             float2 *stats = reinterpret_cast<float2 *>(tile1);
             __syncthreads();
             if (wk > 0) {
-                float *to = lds + ((wk - 1) * WR + wr) * WAVE;
-#pragma unroll
-                for (int dt = 0; dt < DT; ++dt)
-#pragma unroll
-                    for (int r = 0; r < 16; ++r) to[(dt * 16 + r) * 64 + lane] = acc[dt][r];
+                put(lds + ((wk - 1) * WR + wr) * WAVE, lane, acc);
                 stats[wave * 64 + lane] = make_float2(m, l);
             }
             __syncthreads();
@@ -702,38 +745,39 @@ template <typename S> __global__ __launch_bounds__(S::NT, S::HD <= 128 && sizeof
 #pragma unroll
                     for (int dt = 0; dt < DT; ++dt)
 #pragma unroll
-                        for (int r = 0; r < 16; ++r) acc[dt][r] = acc[dt][r] * by + from[(dt * 16 + r) * 64 + lane] * oby;
+                        for (int j = 0; j < 4; ++j) {
+                            const f32x4 y = *reinterpret_cast<const f32x4 *>(from + ((dt * 4 + j) * 64 + lane) * 4);
+#pragma unroll
+                            for (int r = 0; r < 4; ++r) acc[dt][4 * j + r] = acc[dt][4 * j + r] * by + y[r] * oby;
+                        }
                 }
             }
         }
         const bool begins = t0 == 0, ends = t1 == tiles;
         if (wk == 0 && some) {
-            if (begins && ends && w.c.shared_tiles == 0) {
+            if (begins && ends && w->c.shared_tiles == 0) {
                 if (live) {
-                    T *o = out_row<T>(a, row_b, head, node);
+                    T *o = out_row<T>(w->a, row_b, head, node);
                     const float by = 1.0f / l;
 #pragma unroll
                     for (int dt = 0; dt < DT; ++dt) store_row<T>(o, dt, hg, acc[dt], by);
                 }
             } else {
-                const int64_t unit = shared ? (int64_t)h * w.c.shared_units + rt
-                                            : (int64_t)a.H_kv * w.c.shared_units + ((int64_t)b * a.H_kv + h) * w.c.units + rt;
-                const int64_t slot = slot_of(w.c.groups, unit, begins, ends, g);
-                float *to = w.part + (slot * WR + wr) * (32 * S::HD);
-#pragma unroll
-                for (int dt = 0; dt < DT; ++dt)
-#pragma unroll
-                    for (int r = 0; r < 16; ++r) to[(dt * 16 + r) * 64 + lane] = acc[dt][r];
-                if (hg == 0) w.ml[slot * RT + wr * 32 + lane] = make_float2(m == -INFINITY ? -INFINITY : m * c, l);
+                const int H = w->a.H_kv;
+                const int64_t unit = shared ? (int64_t)h * w->c.shared_units + rt
+                                            : (int64_t)H * w->c.shared_units + ((int64_t)b * H + h) * w->c.units + rt;
+                const int64_t slot = slot_of(w->c.groups, unit, begins, ends, g);
+                put(w->part + (slot * WR + wr) * (32 * S::HD), lane, acc);
+                if (hg == 0) w->ml[slot * RT + wr * 32 + lane] = make_float2(m == -INFINITY ? -INFINITY : m * c, l);
             }
         }
 
         left -= t1 - t0;
-        if (left <= 0 || !w.c.groups) return;
+        if (left <= 0 || !w->c.groups) return;
         t0 = 0;                                          // the next unit: row tiles, then heads, then sequences
-        if (++rt < (shared ? w.c.shared_units : w.c.units)) continue;
+        if (++rt < (shared ? w->c.shared_units : w->c.units)) continue;
         rt = 0;
-        if (++h < a.H_kv) continue;
+        if (++h < w->a.H_kv) continue;
         h = 0;
         ++b;
     }
@@ -793,9 +837,13 @@ template <typename S> __global__ __launch_bounds__(256) void join_kernel(Work w)
                 const float2 ml = w.ml[at * RT + span[k].lane];
                 const float by = ml.x == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(ml.x - top);
                 sum += by * ml.y;
-                const float *from = w.part + ((at * S::WR + span[k].lane / 32) * DT + dt) * 1024 + hg * 32 + span[k].lane % 32;
+                const float *from = w.part + ((at * S::WR + span[k].lane / 32) * DT + dt) * 1024 + (hg * 32 + span[k].lane % 32) * 4;
 #pragma unroll
-                for (int j = 0; j < 16; ++j) x[j] += by * from[j * 64];
+                for (int j = 0; j < 4; ++j) {
+                    const f32x4 y = *reinterpret_cast<const f32x4 *>(from + j * 256);
+#pragma unroll
+                    for (int r = 0; r < 4; ++r) x[4 * j + r] += by * y[r];
+                }
             }
 #pragma unroll
     for (int j = 0; j < 16; ++j) sums[wave][j][lane] = x[j];
@@ -885,7 +933,7 @@ template <typename F> auto choose(int rows, int d, int rot, bool f32, F &&f) {
     if (f32) {
         if (d == 64) return rows <= 32 ? f(Shape<float, 64, 1, 4, 128, 8>{}) : f(Shape<float, 64, 4, 1, 128, 8>{});
         if (d == 128) return rows <= 32 ? f(Shape<float, 128, 1, 2, 64, 16>{}) : f(Shape<float, 128, 4, 1, 64, 16>{});
-        return rows <= 32 ? f(Shape<float, 256, 1, 1, 32, 32>{}) : f(Shape<float, 256, 4, 1, 32, 32>{});
+        return rows <= 32 ? f(Shape<float, 256, 1, 1, 32, 32>{}) : f(Shape<float, 256, 2, 1, 32, 32>{});
     }
     if (d == 64) {
         if (rows <= 32) return f(Shape<__bf16, 64, 1, 4, 128, 4>{});
