@@ -25,6 +25,7 @@
 #include "mfma16.h"
 #include "rotate.h"
 
+#include <algorithm>
 #include <type_traits>
 
 namespace treewy {
@@ -55,11 +56,15 @@ template <typename T_, int HD_, int WR_, int WK_, int KT_, int TURN_> struct Sha
     static constexpr int E = 16 / (int)sizeof(T), GRAN = HD / E, STEPS = GRAN / 2, DT = HD / 32;
     static constexpr int TURN = TURN_, LO = sizeof(T) == 2 ? TURN : 0;
     static constexpr int TILE = KT * GRAN;               // granules of a tile's keys (and of its values)
-    static constexpr int LOADS = TILE / 64;              // wave-wide loads of them
-    static constexpr bool Q_FIRST = RT * (GRAN + (LO > 0 ? 2 * TURN : 0)) > 2 * TILE;    // queries need both tiles' LDS on their way
-    static_assert(RT * GRAN <= 2 * TILE && RT * 2 * TURN <= 2 * TILE, "queries fit there");
-    static_assert(KT % (32 * WK) == 0 && LOADS % WAVES == 0, "every wave has as much");
-    static_assert((WK - 1) * WR * 32 * HD * 4 <= 2 * TILE * 16, "key groups meet in one tile's LDS");
+    static constexpr int OCCUPANCY = NT >= 512 || (HD <= 128 && sizeof(T) == 2 && 4 * TILE * 16 <= 80 * 1024) ? 2 : 1;
+    static constexpr int PAIRS = TILE / 64 / WAVES;      // loads of keys (and of values) that a wave has of a tile
+    static constexpr bool REST_LDS = OCCUPANCY == 2 && HD == 256;     // the queries' second parts stay in LDS (registers are short)
+    static constexpr bool Q_FIRST = RT * (GRAN + (LO > 0 && !REST_LDS ? 2 * TURN : 0)) > 2 * TILE;    // queries need both tiles' LDS on their way
+    static constexpr bool Q_BOTH = RT * GRAN > 2 * TILE; // the second half of the rows by way of the first tile
+    static_assert(RT * GRAN <= 4 * TILE && (REST_LDS || RT * (GRAN + 2 * TURN) <= 4 * TILE) && (REST_LDS || !Q_BOTH), "queries fit there");
+    static_assert(KT % (32 * WK) == 0 && KT % (8 * WAVES) == 0, "every wave has as much");
+    static constexpr int MEET = ((WK - 1) * WR * 32 * HD * 4 + 2 * TILE * 16 - 1) / (2 * TILE * 16);     // passes in which key
+    static_assert(WK == 1 || DT % (MEET > 0 ? MEET : 1) == 0, "groups meet in one tile's LDS");          // groups meet
     static_assert(128 % KT == 0, "shared keys end with a tile");
 };
 
@@ -87,16 +92,16 @@ __host__ __device__ inline int draft_tiles_of(int unit, int RT, int KT, int G, i
     return ((last < N ? last : N - 1) + KT) / KT;        // nodes after a row tile's last are nobody's ancestors in it
 }
 
-// Where a workgroup begins in the list, and how many tiles it has.
+// Where a workgroup begins in the list, and how many tiles it has (0: none).
 struct Start {
-    int b, h, rt, t0, tiles, pad[3];                     // b = -1: shared keys, rt among a head's shared units
-};
+    int b, h, rt, t0, tiles, group, longest, pad;        // b = -1: shared keys, rt among a head's shared units; group: its place
+};                                                       // in the list; longest: a sequence with the most cached tokens
 
 // What the first launch leaves in the workspace (pointers into it).
 struct Prepared {
     int64_t *first;                                      // [B + 1] first tile of each sequence
-    Start *start;                                        // [groups]
-    int *info;                                           // groups that have tiles, a sequence with the most cached tokens
+    Start *start;                                        // [workgroups of the kernel]
+    int *info;                                           // groups that have tiles
     int *depth;                                          // [B][N] ancestors
     uint32_t *sees;                                      // [B][N][words] ancestors and self, a bit each (null: a chain)
     uint8_t *odd;                                        // [B][H_kv][N] whether a node's values hold an infinity or NaN
@@ -193,12 +198,22 @@ __device__ void make_list(const Work &w, int RT, int KT) {
     }
     if (tid == 0) w.p.first[a.B] = total;
     const int groups = (int)min((int64_t)w.c.groups, total);
-    if (tid == 0) w.p.info[0] = groups, w.p.info[1] = who[THREADS - 1];
+    if (tid == 0) w.p.info[0] = groups;
     __threadfence_block();
     __syncthreads();
-    for (int g = tid; g < groups; g += THREADS) {
-        const int64_t x = first_of(total, groups, g);
+    // Consecutive parts on one XCD (workgroups go to the eight in turn): row tiles that read the same keys meet in its L2.  Where
+    // there are fewer tiles than workgroups they have one each, on all XCDs.
+    const int per_xcd = w.c.groups / 8;
+    for (int i = tid; i < w.c.groups; i += THREADS) {
+        const int g = groups < w.c.groups || i >= per_xcd * 8 ? i : (i & 7) * per_xcd + (i >> 3);
         Start s{};
+        if (g >= groups) {
+            w.p.start[i] = s;
+            continue;
+        }
+        const int64_t x = first_of(total, groups, g);
+        s.group = g;
+        s.longest = who[THREADS - 1];
         s.tiles = (int)(first_of(total, groups, g + 1) - x);
         if (x < shared) {
             const int n = (int)(x / w.c.shared_tiles);
@@ -225,7 +240,7 @@ __device__ void make_list(const Work &w, int RT, int KT) {
             }
             s.t0 = left;
         }
-        w.p.start[g] = s;
+        w.p.start[i] = s;
     }
 }
 
@@ -334,7 +349,7 @@ __device__ __forceinline__ float other_half(float x) { return __shfl_xor(x, 32);
 __device__ __forceinline__ int uniform(int x) { return __builtin_amdgcn_readfirstlane(x); }
 
 // A wave's O^T: [HD/32][4][64 lanes][4], the four values of a row that follow one another side by side.
-template <int DT> __device__ __forceinline__ void put(float *to, int lane, const f32x16 (&x)[DT]) {
+template <int DT> __device__ __forceinline__ void put(float *to, int lane, const f32x16 *x) {
 #pragma unroll
     for (int dt = 0; dt < DT; ++dt)
 #pragma unroll
@@ -357,29 +372,25 @@ __device__ __forceinline__ Args *arguments() {
 // understands: after it, reads of one tile do not wait for the loads of the next.)
 __device__ __forceinline__ void loads_done() { __builtin_amdgcn_s_waitcnt(0x0f70); }
 
-template <typename S> __global__ __launch_bounds__(S::NT, S::HD <= 128 && sizeof(typename S::T) == 2 ? 2 : 1) void attend_kernel(Work) {
+template <typename S> __global__ __launch_bounds__(S::NT, S::OCCUPANCY) void attend_kernel(Work) {
     using T = typename S::T;
     constexpr int KT = S::KT, RT = S::RT, GRAN = S::GRAN, E = S::E, ROW = 16 * GRAN, WK = S::WK, WR = S::WR, DT = S::DT;
-    constexpr int NB = KT / (32 * WK);                   // blocks of 32 keys that a wave has of a tile
+    constexpr int BLOCKS = KT / (32 * WK);               // blocks of 32 keys that a wave has of a tile,
+    constexpr int NB = S::REST_LDS || BLOCKS == 1 ? 1 : 2;            // and how many it takes at once
     constexpr int PER_LOAD = 64 / GRAN;                  // rows of one load
     constexpr bool BF = sizeof(T) == 2;
-    __shared__ uint4 tile0[2 * S::TILE], tile1[2 * S::TILE];
+    __shared__ uint4 tile0[2 * S::TILE], tile1[2 * S::TILE], rests[S::REST_LDS ? RT * 2 * S::TURN : 1];
     const int lane = threadIdx.x & 63, wave = uniform(threadIdx.x >> 6), hg = lane >> 5, wr = wave / WK, wk = wave % WK;
     Args *w = arguments();
-    // Consecutive parts of the list on one XCD (workgroups go to the eight in turn): row tiles that read the same keys meet in its L2.
-    const unsigned per = gridDim.x / 8;
-    int g = blockIdx.x;
-    if (blockIdx.x < per * 8) g = (int)((blockIdx.x & 7u) * per + (blockIdx.x >> 3));
-
-    int b, h, rt, t0, left, longest = 0;
+    int b, h, rt, t0, left, g = blockIdx.x, longest = 0;
     if (w->c.groups) {
-        const int groups = uniform(w->p.info[0]);
-        longest = uniform(w->p.info[1]);
-        if (groups < w->c.groups) g = blockIdx.x;        // (fewer tiles than workgroups: one each, on all XCDs)
-        if (g >= groups) return;
         const Start s = w->p.start[g];
-        b = uniform(s.b), h = uniform(s.h), rt = uniform(s.rt), t0 = uniform(s.t0), left = uniform(s.tiles);
-    } else {                                             // one unit
+        left = uniform(s.tiles);
+        if (left == 0) return;
+        b = uniform(s.b), h = uniform(s.h), rt = uniform(s.rt), t0 = uniform(s.t0), g = uniform(s.group), longest = uniform(s.longest);
+    } else {                                             // one unit, those of a head's keys on one XCD (see make_list)
+        const unsigned per = gridDim.x / 8;
+        if (blockIdx.x < per * 8) g = (int)((blockIdx.x & 7u) * per + (blockIdx.x >> 3));
         b = g / (w->a.H_kv * w->c.units);
         const int n = g - b * w->a.H_kv * w->c.units;
         h = n / w->c.units;
@@ -388,20 +399,8 @@ template <typename S> __global__ __launch_bounds__(S::NT, S::HD <= 128 && sizeof
         left = INT32_MAX;
     }
 
-    // Addresses in a tile's LDS, the same for every tile: keys of the lane's row from its granule hg on (granule 2 i + hg is
-    // i << 5 away by exclusive or), values by the four keys that a lane reads at once (32 columns further: dt << 6, too).
-    const int row_at = (lane & 31) * ROW + place<GRAN>(lane & 31, hg) * 16;
-    int val_at[2] = {};
-    if constexpr (BF) {
-        const int j = (lane >> 2) & 3, y = lane & 3, c16 = (lane >> 4) & 1;
-#pragma unroll
-        for (int e = 0; e < 2; ++e) {
-            const int r = 8 * e + 4 * hg + j;
-            val_at[e] = r * ROW + place<GRAN>(r, c16 * 2 + (y >> 1)) * 16 + (y & 1) * 8;
-        }
-    } else {
-        val_at[0] = 4 * hg * ROW + place<GRAN>(4 * hg, (lane & 31) / 4) * 16 + (lane & 3) * 4;
-    }
+    const uint32_t load_at = (lane / GRAN) * ROW + place<GRAN>(lane / GRAN, lane % GRAN) * 16;      // a lane's place in a load's rows
+
     while (true) {
         w = arguments();
         const auto &a = w->a;
@@ -422,60 +421,75 @@ template <typename S> __global__ __launch_bounds__(S::NT, S::HD <= 128 && sizeof
         const char *vp = (const char *)a.v_pages + ((int64_t)h * ROW << log2_page);
         const int64_t draft = ((int64_t)own_b * a.H_kv + h) * N * ROW;
         const char *dk = (const char *)w->p.k + draft, *dv = (const char *)w->p.v + draft;
-        const uint32_t *tree = a.parent ? w->p.sees : nullptr;
+        const uint32_t *tree = a.parent && !shared ? w->p.sees + (int64_t)b * N * w->words : nullptr;
         const int words = w->words;
 
-        // Lane p: the p-th page of tile t's tokens, -1 where there is none or an invalid one.
-        auto pages_of = [&](int t) {
-            const int key0 = first_key + t * KT, end = min(key0 + KT, len), page = (key0 >> log2_page) + lane;
-            int id = -1;
-            if (t < old_tiles && page <= (end - 1) >> log2_page) {
-                id = table[page];
-                if ((unsigned)id >= (unsigned)n_pages) {
-                    id = -1;
-                    Args *w = arguments();
-                    for (int s = shared ? 0 : b; s < (shared ? w->a.B : b + 1); ++s)
-                        if (cached(w->a, s) > page << log2_page) flag_error(w->a.err, s, TREEWY_FLAG_BAD_PAGE);
-                }
-            }
-            return id;
-        };
-        auto pages_in = [&](int t) {                     // how many that is
+        auto pages_in = [&](int t) {                     // pages of tile t's tokens
             const int key0 = first_key + t * KT, end = min(key0 + KT, len);
             return t < old_tiles && end > key0 ? ((end - 1) >> log2_page) - (key0 >> log2_page) + 1 : 0;
         };
+        // Lane p: the table's entry for the p-th page of tile t's tokens, -1 where there is none.
+        auto entries_of = [&](int t) {
+            const int key0 = first_key + t * KT, end = min(key0 + KT, len), page = (key0 >> log2_page) + lane;
+            return t < old_tiles && page <= (end - 1) >> log2_page ? table[page] : -1;
+        };
+        // The same with invalid pages as -1.  (Apart from the load, which is under way while a tile is computed; a look at its
+        // result there would wait for that tile's loads as well.)
+        auto checked = [&](int id, int t) {
+            if ((unsigned)id < (unsigned)n_pages) return id;
+            const int page = ((first_key + t * KT) >> log2_page) + lane;
+            if (lane < pages_in(t)) {
+                Args *w = arguments();
+                for (int s = shared ? 0 : b; s < (shared ? w->a.B : b + 1); ++s)
+                    if (cached(w->a, s) > page << log2_page) flag_error(w->a.err, s, TREEWY_FLAG_BAD_PAGE);
+            }
+            return -1;
+        };
+        // Whether tile t is whole: no row of it masked.
+        auto whole_tile = [&](int t, int pages) {
+            const bool old = t < old_tiles;
+            const int key0 = old ? first_key + t * KT : (t - old_tiles) * KT, end = old ? len : N;
+            return key0 + KT <= end && (!old || __ballot(lane < pages_in(t) && pages < 0) == 0);
+        };
+        // Rows r8 .. r8 + 7 of tile t: in one page, so that all but a lane's place in them is scalar.  (place() of a row is linear
+        // in the row's bits: what depends on the lane is formed once.)
+        struct Rows {
+            const char *k, *v;
+            bool none;
+        };
+        auto rows_at = [&](int t, int r8, int pages) {
+            const bool old = t < old_tiles;
+            const int key0 = old ? first_key + t * KT : (t - old_tiles) * KT, key = key0 + r8;
+            Rows x{dk + key * ROW, dv + key * ROW, false};
+            if (old) {
+                const int id = __builtin_amdgcn_readlane(pages, (key >> log2_page) - (key0 >> log2_page));
+                const int64_t at = max(id, 0) * page_bytes + (key & page_rows) * ROW;
+                x = Rows{kp + at, vp + at, id < 0};
+            }
+            return x;
+        };
+        constexpr int EIGHT = 8 / PER_LOAD;              // loads of eight rows
         // Issues the loads of tile t into `tile`.
         auto fetch = [&](uint4 *tile, int t, int pages) {
             const bool old = t < old_tiles;
             const int key0 = old ? first_key + t * KT : (t - old_tiles) * KT, end = old ? len : N;
-            const bool whole = key0 + KT <= end && (!old || __ballot(lane < pages_in(t) && pages < 0) == 0);
 #pragma unroll 1
-            for (int load = wave; load < S::LOADS; load += S::WAVES) {
-                const int r0 = load * PER_LOAD, r = r0 + lane / GRAN;
-                const int off = (lane / GRAN) * ROW + place<GRAN>(r, lane % GRAN) * 16;
-                const int key = key0 + r0;               // (the rows of a load are in one page)
-                const char *k, *v;
-                bool none = false;
-                if (old) {
-                    const int id = __builtin_amdgcn_readlane(pages, (key >> log2_page) - (key0 >> log2_page));
-                    const int64_t at = max(id, 0) * page_bytes + (key & page_rows) * ROW;
-                    k = kp + at;
-                    v = vp + at;
-                    none = id < 0;
-                } else {
-                    k = dk + key * ROW;
-                    v = dv + key * ROW;
+            for (int r8 = wave * 8; r8 < KT; r8 += S::WAVES * 8) {
+                const Rows x = rows_at(t, r8, pages);
+#pragma unroll 1
+                for (int i = 0; i < EIGHT; ++i) {
+                    const int r0 = r8 + i * PER_LOAD;
+                    const uint32_t off = load_at ^ (place<GRAN>(r0, 0) * 16);
+                    global_void *k = (global_void *)(x.k + i * PER_LOAD * ROW + off), *v = (global_void *)(x.v + i * PER_LOAD * ROW + off);
+                    if (x.none || key0 + r0 + lane / GRAN >= end) k = v = (global_void *)(zero_row + lane % GRAN);
+                    __builtin_amdgcn_global_load_lds(k, (lds_void *)(tile + r0 * GRAN), 16, 0, 0);
+                    __builtin_amdgcn_global_load_lds(v, (lds_void *)(tile + S::TILE + r0 * GRAN), 16, 0, 0);
                 }
-                k += off;
-                v += off;
-                if (!whole && (none || key0 + r >= end)) k = v = (const char *)(zero_row + lane % GRAN);
-                __builtin_amdgcn_global_load_lds((global_void *)k, (lds_void *)(tile + load * 64), 16, 0, 0);
-                __builtin_amdgcn_global_load_lds((global_void *)v, (lds_void *)(tile + S::TILE + load * 64), 16, 0, 0);
             }
         };
 
         __syncthreads();                                 // (the last part's LDS is read)
-        int pages = pages_of(t0), ahead = pages_of(t0 + 1);
+        int pages = checked(entries_of(t0), t0), ahead = entries_of(t0 + 1);
         if constexpr (!S::Q_FIRST) fetch(tile0, t0, pages);
 
         // the lane's query row
@@ -487,13 +501,13 @@ template <typename S> __global__ __launch_bounds__(S::NT, S::HD <= 128 && sizeof
         // Queries go through LDS: a row's granules are read side by side, and the rotation is one short loop (unrolled over a
         // lane's own granules it was a third of the kernel's instructions, each run once and most of them not in the
         // instruction cache).
-        uint4 q[S::STEPS], q_rest[S::LO > 0 ? S::LO : 1];
+        uint4 q[S::STEPS], q_rest[S::LO > 0 && !S::REST_LDS ? S::LO : 1];
         {
             constexpr int HALF = GRAN / 2, ROWS = 64 / HALF, TG = 2 * S::TURN;
-            uint4 *hi = tile1 + wr * 32 * GRAN, *rest = (S::Q_FIRST ? tile0 : tile1 + RT * GRAN) + wr * 32 * TG;
+            uint4 *hi = (S::Q_BOTH && wr >= WR / 2 ? tile0 - WR / 2 * 32 * GRAN : tile1) + wr * 32 * GRAN, *rest = (S::REST_LDS ? rests : S::Q_FIRST ? tile0 : tile1 + RT * GRAN) + wr * 32 * TG;
             const int64_t src = row_b * a.qs.seq + head * a.qs.head + node * a.qs.token;
             const int half = a.rot / (2 * E);
-            const int at = a.rot ? position(a, row_len, w->p.depth[(int64_t)row_b * N + node], row_b) : 0;
+            const int at = a.rot ? position(a, row_len, a.parent ? w->p.depth[(int64_t)row_b * N + node] : node, row_b) : 0;
             const uint32_t flip = a.scale < 0.0f ? (BF ? 0x80008000u : 0x80000000u) : 0u;
 #pragma unroll 1
             for (int r0 = wk * ROWS; r0 < 32; r0 += WK * ROWS) {
@@ -531,7 +545,7 @@ template <typename S> __global__ __launch_bounds__(S::NT, S::HD <= 128 && sizeof
 #pragma unroll
             for (int i = 0; i < S::STEPS; ++i) q[i] = hi[r * GRAN + place<GRAN>(r, 2 * i + hg)];
 #pragma unroll
-            for (int i = 0; i < S::LO; ++i) q_rest[i] = rest[r * TG + place<TG>(r, 2 * i + hg)];
+            for (int i = 0; i < (S::REST_LDS ? 0 : S::LO); ++i) q_rest[i] = rest[r * TG + place<TG>(r, 2 * i + hg)];
         }
         if constexpr (S::Q_FIRST) {
             __syncthreads();
@@ -543,37 +557,78 @@ template <typename S> __global__ __launch_bounds__(S::NT, S::HD <= 128 && sizeof
 #pragma unroll
         for (int dt = 0; dt < DT; ++dt) acc[dt] = f32x16{};
 
-        auto compute = [&](const uint4 *tile, int t, int now) {
-            const char *kt = reinterpret_cast<const char *>(tile) + wk * 32 * NB * ROW, *vt = kt + S::TILE * 16;
+        // (next: where the loads of tile t + 1 go, a pair at a time between products if `load`: issued all at once they held the
+        // wave up, since the memory pipe takes one in some 50 cycles)
+        auto compute = [&](const uint4 *tile, int t, int now, uint4 *next, bool load) {
+#pragma unroll 1
+          for (int sub = 0; sub < BLOCKS; sub += NB) {
+            const char *kt = reinterpret_cast<const char *>(tile) + (wk * BLOCKS + sub) * 32 * ROW, *vt = kt + S::TILE * 16;
             const bool old = t < old_tiles;
-            // (opaque: addresses are formed where they are used, not kept for all of the loop)
-            const int key_at = opaque(row_at), val0 = opaque(val_at[0]), val1 = BF ? opaque(val_at[BF]) : 0;
-            const int first = (old ? first_key + t * KT : (t - old_tiles) * KT) + wk * 32 * NB;
+            // Addresses in a tile's LDS: keys of the lane's row from its granule hg on (granule 2 i + hg is i << 5 away by
+            // exclusive or), values by the four keys that a lane reads at once (32 columns further: dt << 6, too).  Formed
+            // anew for each tile (opaque): kept over the loop they were spilled.
+            const int ln = opaque(lane), hf = ln >> 5, key_at = (ln & 31) * ROW + place<GRAN>(ln & 31, hf) * 16;
+            const int rest_at = (wr * 32 + (ln & 31)) * 2 * S::TURN;
+            const int place_at = (ln / GRAN) * ROW + place<GRAN>(ln / GRAN, ln % GRAN) * 16;   // (load_at)
+            int val0, val1 = 0;
+            if constexpr (BF) {
+                const int j = (ln >> 2) & 3, y = ln & 3, c16 = (ln >> 4) & 1, r0 = 4 * hf + j;
+                val0 = r0 * ROW + place<GRAN>(r0, c16 * 2 + (y >> 1)) * 16 + (y & 1) * 8;
+                val1 = (val0 ^ (place<GRAN>(8, 0) * 16)) + 8 * ROW;
+            } else {
+                val0 = 4 * hf * ROW + place<GRAN>(4 * hf, (ln & 31) / 4) * 16 + (ln & 3) * 4;
+            }
+            const int first = (old ? first_key + t * KT : (t - old_tiles) * KT) + (wk * BLOCKS + sub) * 32;
             // Both products read their operands a group ahead of the group that they multiply; sched_barrier keeps it so (left
             // alone the compiler reads each operand right before its use).
             f32x16 x[NB];
 #pragma unroll
             for (int n = 0; n < NB; ++n) x[n] = f32x16{};
-            constexpr int KG = S::STEPS / 2;             // groups of two steps
-            uint4 kf[2][2 * NB];
+            constexpr int STEP = S::REST_LDS ? 1 : 2, KG = S::STEPS / STEP;             // steps of a group
+            constexpr int KA = S::REST_LDS ? 3 : 1;      // groups that are read ahead: a read takes longer than two products
+            uint4 kf[KA + 1][STEP * NB], rf[2][S::REST_LDS ? STEP : 1];
+            auto read_rests = [&](int group) {
+                if constexpr (S::REST_LDS)
+#pragma unroll
+                    for (int j = 0; j < STEP; ++j)
+                        if (STEP * group + j < S::LO) rf[group & 1][j] = rests[rest_at + place<2 * S::TURN>(ln & 31, 2 * (STEP * group + j) + hf)];
+            };
             auto read_keys = [&](int group) {
 #pragma unroll
-                for (int j = 0; j < 2; ++j)
+                for (int j = 0; j < STEP; ++j)
 #pragma unroll
                     for (int n = 0; n < NB; ++n)
-                        kf[group & 1][j * NB + n] = *reinterpret_cast<const uint4 *>(kt + n * 32 * ROW + (key_at ^ ((2 * group + j) << 5)));
+                        kf[group % (KA + 1)][j * NB + n] = *reinterpret_cast<const uint4 *>(kt + n * 32 * ROW + (key_at ^ ((STEP * group + j) << 5)));
             };
-            read_keys(0);
+            Rows rows{};
+            read_rests(0);
+#pragma unroll
+            for (int group = 0; group < KA; ++group) read_keys(group);
 #pragma unroll
             for (int group = 0; group < KG; ++group) {
-                if (group + 1 < KG) read_keys(group + 1);
+                if (group + KA < KG) read_keys(group + KA);
+                if (group + 1 < KG) read_rests(group + 1);
+                __builtin_amdgcn_sched_barrier(0);
+                if (load && sub == 0) {
+                    constexpr int EACH = (S::PAIRS + KG - 1) / KG;
+#pragma unroll
+                    for (int pair = group * EACH; pair < S::PAIRS && pair < (group + 1) * EACH; ++pair) {
+                        const int i = pair % EIGHT, r8 = (pair / EIGHT * S::WAVES + wave) * 8, r0 = r8 + i * PER_LOAD;
+                        if (i == 0) rows = rows_at(t + 1, r8, pages);
+                        const uint32_t off = (uint32_t)opaque(place_at) ^ (place<GRAN>(r0, 0) * 16);
+                        __builtin_amdgcn_global_load_lds((global_void *)(rows.k + i * PER_LOAD * ROW + off),
+                                                         (lds_void *)(next + r0 * GRAN), 16, 0, 0);
+                        __builtin_amdgcn_global_load_lds((global_void *)(rows.v + i * PER_LOAD * ROW + off),
+                                                         (lds_void *)(next + S::TILE + r0 * GRAN), 16, 0, 0);
+                    }
+                }
                 __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-                for (int j = 0; j < 2; ++j) {
-                    const int i = 2 * group + j;
+                for (int j = 0; j < STEP; ++j) {
+                    const int i = STEP * group + j;
 #pragma unroll
                     for (int n = 0; n < NB; ++n) {
-                        const uint4 k = kf[group & 1][j * NB + n];
+                        const uint4 k = kf[group % (KA + 1)][j * NB + n];
                         if constexpr (BF) {
                             x[n] = mma(__builtin_bit_cast(bf16x8, k), __builtin_bit_cast(bf16x8, q[i]), x[n]);
                         } else {
@@ -585,24 +640,23 @@ template <typename S> __global__ __launch_bounds__(S::NT, S::HD <= 128 && sizeof
                     if (i < S::LO)
 #pragma unroll
                         for (int n = 0; n < NB; ++n)
-                            x[n] = mma(__builtin_bit_cast(bf16x8, kf[group & 1][j * NB + n]),
-                                       __builtin_bit_cast(bf16x8, q_rest[i < S::LO ? i : 0]), x[n]);
+                            x[n] = mma(__builtin_bit_cast(bf16x8, kf[group % (KA + 1)][j * NB + n]),
+                                       __builtin_bit_cast(bf16x8, S::REST_LDS ? rf[group & 1][S::REST_LDS ? j : 0] : q_rest[S::REST_LDS || i >= S::LO ? 0 : i]),
+                                       x[n]);
                 }
                 __builtin_amdgcn_sched_barrier(0);
             }
-            constexpr int VG = BF ? NB * DT : 1;         // groups of two products of 16 keys with 32 values
-            s16x4 vf[2][4];
-            auto read_values = [&](int group) {
+            constexpr int VG = BF ? 2 * NB * DT : 1, VA = S::REST_LDS ? 3 : 5;           // products of 16 keys with 32 values; read ahead
+            s16x4 vf[VA + 1][2];
+            auto read_values = [&](int i) {
+                const int s = i / DT, dt = i % DT;
 #pragma unroll
-                for (int j = 0; j < 2; ++j) {
-                    const int s = (2 * group + j) / DT, dt = (2 * group + j) % DT;
-#pragma unroll
-                    for (int e = 0; e < 2; ++e)
-                        vf[group & 1][2 * j + e] =
-                            __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4 *)(vt + s * 16 * ROW + ((e ? val1 : val0) ^ (dt << 6))));
-                }
+                for (int e = 0; e < 2; ++e)
+                    vf[i % (VA + 1)][e] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4 *)(vt + s * 16 * ROW + ((e ? val1 : val0) ^ (dt << 6))));
             };
-            if constexpr (BF) read_values(0);
+            if constexpr (BF)
+#pragma unroll
+                for (int i = 0; i < (S::REST_LDS ? 1 : 2); ++i) read_values(i);
             // What the row does not see: keys past its limit or of invalid pages, nodes that are not its ancestors.
             const uint64_t bad = old ? __ballot(lane < pages_in(t) && now < 0) : 0;
             if (!old || bad || __any(first + 32 * NB > limit)) {
@@ -610,7 +664,7 @@ template <typename S> __global__ __launch_bounds__(S::NT, S::HD <= 128 && sizeof
                 for (int n = 0; n < NB; ++n) {
                     const int key = first + 32 * n, have = old ? limit - key : node + 1 - key;
                     uint32_t sees = have >= 32 ? ~0u : have <= 0 ? 0u : (1u << have) - 1u;
-                    if (!old && tree) sees = key < N ? tree[((int64_t)b * N + node) * words + key / 32] : 0u;
+                    if (!old && tree) sees = key < N ? tree[(uint32_t)(node * words + key / 32)] : 0u;
                     if (bad)
 #pragma unroll 1
                         for (int i = 0; i < 32; ++i) {
@@ -655,15 +709,13 @@ template <typename S> __global__ __launch_bounds__(S::NT, S::HD <= 128 && sizeof
                     p[s] = __builtin_bit_cast(bf16x8, pk);
                 }
 #pragma unroll
-                for (int group = 0; group < VG; ++group) {
-                    if (group + 1 < VG) read_values(group + 1);
-                    __builtin_amdgcn_sched_barrier(0);
+                for (int i = S::REST_LDS ? 1 : 2; i < VA; ++i) read_values(i);
 #pragma unroll
-                    for (int j = 0; j < 2; ++j) {
-                        const int s = (2 * group + j) / DT, dt = (2 * group + j) % DT;
-                        acc[dt] = mma(both8(__builtin_bit_cast(uint2, vf[group & 1][2 * j]), __builtin_bit_cast(uint2, vf[group & 1][2 * j + 1])),
-                                      p[s], acc[dt]);
-                    }
+                for (int i = 0; i < VG; ++i) {
+                    if (i + VA < VG) read_values(i + VA);
+                    __builtin_amdgcn_sched_barrier(0);
+                    acc[i % DT] = mma(both8(__builtin_bit_cast(uint2, vf[i % (VA + 1)][0]), __builtin_bit_cast(uint2, vf[i % (VA + 1)][1])),
+                                      p[i / DT], acc[i % DT]);
                     __builtin_amdgcn_sched_barrier(0);
                 }
             } else {
@@ -678,17 +730,20 @@ template <typename S> __global__ __launch_bounds__(S::NT, S::HD <= 128 && sizeof
                             acc[dt] = mma_f32(y, x[n][r], acc[dt]);
                         }
             }
+          }
         };
         auto step = [&](const uint4 *here, uint4 *next, int t) {
             loads_done();
             __syncthreads();
             const int now = pages;
-            pages = ahead;
+            bool load = false;
             if (t + 1 < t1) {
-                fetch(next, t + 1, pages);
-                ahead = pages_of(t + 2);
+                pages = checked(ahead, t + 1);
+                load = some && whole_tile(t + 1, pages);
+                if (!load) fetch(next, t + 1, pages);
             }
-            if (some) compute(here, t, now);
+            if (some) compute(here, t, now, next, load);
+            if (t + 1 < t1) ahead = entries_of(t + 2);
         };
         for (int t = t0; t < t1; t += 2) {
             step(tile0, tile1, t);
@@ -723,35 +778,42 @@ template <typename S> __global__ __launch_bounds__(S::NT, S::HD <= 128 && sizeof
         // the key groups of each row group meet in its first wave
         l += other_half(l);
         if constexpr (WK > 1) {
-            constexpr int WAVE = DT * 16 * 64;
+            constexpr int PART = DT / S::MEET, WAVE = PART * 16 * 64;
             float *lds = reinterpret_cast<float *>(tile0);
             float2 *stats = reinterpret_cast<float2 *>(tile1);
             __syncthreads();
-            if (wk > 0) {
-                put(lds + ((wk - 1) * WR + wr) * WAVE, lane, acc);
-                stats[wave * 64 + lane] = make_float2(m, l);
-            }
+            if (wk > 0) stats[wave * 64 + lane] = make_float2(m, l);
             __syncthreads();
-            if (wk == 0) {
-#pragma unroll 1
-                for (int k = 1; k < WK; ++k) {
-                    const float2 o = stats[(wave + k) * 64 + lane];
-                    const float to = fmaxf(m, o.x);
-                    const float by = m == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f((m - to) * c);
-                    const float oby = o.x == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f((o.x - to) * c);
-                    const float *from = lds + ((k - 1) * WR + wr) * WAVE;
-                    m = to;
-                    l = l * by + o.y * oby;
+            float to = m, sum = 0.0f, by[WK];
 #pragma unroll
-                    for (int dt = 0; dt < DT; ++dt)
+            for (int k = 1; k < WK; ++k) to = fmaxf(to, stats[(wr * WK + k) * 64 + lane].x);
+#pragma unroll
+            for (int k = 0; k < WK; ++k) {
+                const float2 o = k ? stats[(wr * WK + k) * 64 + lane] : make_float2(m, l);
+                by[k] = o.x == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f((o.x - to) * c);
+                sum += o.y * by[k];
+            }
+#pragma unroll
+            for (int part = 0; part < S::MEET; ++part) {
+                if (part) __syncthreads();
+                if (wk > 0) put<PART>(lds + ((wk - 1) * WR + wr) * WAVE, lane, acc + part * PART);
+                __syncthreads();
+                if (wk == 0)
+#pragma unroll
+                    for (int dt = part * PART; dt < (part + 1) * PART; ++dt)
 #pragma unroll
                         for (int j = 0; j < 4; ++j) {
-                            const f32x4 y = *reinterpret_cast<const f32x4 *>(from + ((dt * 4 + j) * 64 + lane) * 4);
+                            f32x4 y = f32x4{acc[dt][4 * j], acc[dt][4 * j + 1], acc[dt][4 * j + 2], acc[dt][4 * j + 3]} * by[0];
 #pragma unroll
-                            for (int r = 0; r < 4; ++r) acc[dt][4 * j + r] = acc[dt][4 * j + r] * by + y[r] * oby;
+                            for (int k = 1; k < WK; ++k)
+                                y += *reinterpret_cast<const f32x4 *>(lds + ((k - 1) * WR + wr) * WAVE +
+                                                                      (((dt - part * PART) * 4 + j) * 64 + lane) * 4) * by[k];
+#pragma unroll
+                            for (int r = 0; r < 4; ++r) acc[dt][4 * j + r] = y[r];
                         }
-                }
             }
+            m = to;
+            l = sum;
         }
         const bool begins = t0 == 0, ends = t1 == tiles;
         if (wk == 0 && some) {
@@ -767,7 +829,7 @@ template <typename S> __global__ __launch_bounds__(S::NT, S::HD <= 128 && sizeof
                 const int64_t unit = shared ? (int64_t)h * w->c.shared_units + rt
                                             : (int64_t)H * w->c.shared_units + ((int64_t)b * H + h) * w->c.units + rt;
                 const int64_t slot = slot_of(w->c.groups, unit, begins, ends, g);
-                put(w->part + (slot * WR + wr) * (32 * S::HD), lane, acc);
+                put<DT>(w->part + (slot * WR + wr) * (32 * S::HD), lane, acc);
                 if (hg == 0) w->ml[slot * RT + wr * 32 + lane] = make_float2(m == -INFINITY ? -INFINITY : m * c, l);
             }
         }
@@ -874,7 +936,7 @@ template <typename S> Cut cut(int shared, int N, int B, int H_q, int H_kv) {
         c.shared_tiles = (shared + S::KT - 1) / S::KT;
     }
     const int resident = compute_units() * (4 * S::TILE * 16 > 80 * 1024 ? 1 : 2);
-    if (shared == 0 && all >= 3 * (int64_t)resident) return c;        // enough units to even themselves out
+    if (shared == 0 && all >= 3 * (int64_t)resident) return c;      // enough units to even themselves out
     c.groups = resident;
     c.slots = 2 * (int64_t)resident + (shared > 0 ? (int64_t)H_kv * c.shared_units + all : 0);
     return c;
@@ -892,7 +954,7 @@ template <typename S> size_t lay_out(Work &w, void *workspace) {
     char *k, *v;
     const size_t rows = (size_t)a.B * a.H_kv * a.N;
     take(w.p.first, a.B + 1);
-    take(w.p.info, 2);
+    take(w.p.info, 1);
     take(w.p.start, w.c.groups);
     take(w.p.odd, rows);
     take(w.p.depth, (size_t)a.B * a.N);
@@ -937,15 +999,18 @@ template <typename F> auto choose(int rows, int d, int rot, bool f32, F &&f) {
     }
     if (d == 64) {
         if (rows <= 32) return f(Shape<__bf16, 64, 1, 4, 128, 4>{});
-        return rows <= 64 ? f(Shape<__bf16, 64, 2, 2, 128, 4>{}) : f(Shape<__bf16, 64, 4, 1, 128, 4>{});
+        if (rows <= 64) return f(Shape<__bf16, 64, 2, 2, 128, 4>{});
+        return rows <= 128 ? f(Shape<__bf16, 64, 4, 1, 128, 4>{}) : f(Shape<__bf16, 64, 8, 1, 128, 4>{});
     }
     if (d == 128) {
         if (rows <= 32) return f(Shape<__bf16, 128, 1, 4, 128, 8>{});
-        return rows <= 64 ? f(Shape<__bf16, 128, 2, 2, 128, 8>{}) : f(Shape<__bf16, 128, 4, 1, 64, 8>{});
+        if (rows <= 64) return f(Shape<__bf16, 128, 2, 2, 128, 8>{});
+        return rows <= 128 ? f(Shape<__bf16, 128, 4, 1, 64, 8>{}) : f(Shape<__bf16, 128, 8, 1, 128, 8>{});
     }
     if (rot <= 64) {
         if (rows <= 32) return f(Shape<__bf16, 256, 1, 2, 64, 4>{});
-        return rows <= 64 ? f(Shape<__bf16, 256, 2, 2, 64, 4>{}) : f(Shape<__bf16, 256, 4, 1, 64, 4>{});
+        if (rows <= 64) return f(Shape<__bf16, 256, 2, 2, 64, 4>{});
+        return rows <= 128 ? f(Shape<__bf16, 256, 4, 1, 64, 4>{}) : f(Shape<__bf16, 256, 8, 1, 64, 4>{});
     }
     if (rows <= 32) return f(Shape<__bf16, 256, 1, 2, 64, 16>{});
     return rows <= 64 ? f(Shape<__bf16, 256, 2, 2, 64, 16>{}) : f(Shape<__bf16, 256, 4, 1, 64, 16>{});
@@ -957,7 +1022,12 @@ int shared_used(int shared, int N, int B, int H_q, int H_kv) {
     return B > 1 && N * (H_q / H_kv) <= 64 && N <= 16 ? shared / 128 * 128 : 0;
 }
 
-int rows_of(int shared, int N, int B, int H_q, int H_kv) { return N * (H_q / H_kv) * (shared > 0 ? B : 1); }
+// Rows by which a call's kernel is chosen: those of a sequence, or where keys are shared at most 64 of the batch (the tiles of each
+// sequence's own keys, with few rows, are more).
+int rows_of(int shared, int N, int B, int H_q, int H_kv) {
+    const int rows = N * (H_q / H_kv);
+    return shared > 0 ? std::max(rows, std::min(64, rows * std::min(B, 64))) : rows;
+}
 
 }  // namespace
 
