@@ -4,13 +4,20 @@
 // 2^-40, so that sums of them are exact in any order: histograms by atomics,
 // partial sums of waves and a walk in the order of the vocabulary all agree.
 //
-// The tokens that the filters keep are a prefix of the order (logit down,
-// index up).  It is never sorted: one pass counts tokens and likelihoods by
-// bins of 1/12 octave below the largest, which shows the bin that the prefix
-// ends in, and passes over the digits of that bin's logits narrow it to one
-// logit `cut` and a number of its ties.  A last pass sums what is kept by
-// segments of the vocabulary, and the segment that holds the drawn point is
-// walked by one wave.
+// A workgroup has a row.  The tokens that the filters keep are a prefix of the
+// order (logit down, index up), which is never sorted as a whole:
+//  - The first pass finds the largest logit, of the row and of each thread's
+//    share.  The k-th largest of the 1024 threads' is a bound that at least k
+//    tokens reach, and few more do: the second pass lists those, and all else
+//    is done on the list (top-k up to 512; top-p, whose second pass sums the
+//    row as well, where the list proves to hold enough).
+//  - Where that does not do (a flat row's top-p, thousands of ties), a pass
+//    counts tokens and likelihoods by bins of 1/12 octave below the largest,
+//    which shows the bin that the prefix ends in, passes over the digits of
+//    that bin's logits narrow it to one logit `cut` and a number of its ties,
+//    and a last pass sums what is kept by segments of the vocabulary.  The
+//    segment that holds the drawn point is walked by one wave.  Without top-k
+//    and top-p only this last pass is needed.
 #include "hybrid_launch.h"
 #include "device.h"
 
@@ -23,9 +30,12 @@ typedef unsigned long long u64;
 constexpr int ROW_THREADS = 1024, WAVES = ROW_THREADS / 64;
 constexpr int EACH = 8;                                  // elements of a thread in one step
 constexpr int SEGMENT = 64 * EACH;                       // ... of a wave: one segment of the last pass
-constexpr int MAX_V = 1 << 20;
+constexpr int MAX_V = 1 << 20, MAX_SEGMENTS = MAX_V / SEGMENT + 1;
 constexpr int BINS = 512;                                // 1/12 octave each; 2^-40 is in bin 480
 constexpr float BINS_PER_OCTAVE = 12.0f;
+constexpr int LIST = ROW_THREADS;                        // longest list: a thread per token
+constexpr int MOST_K = 512;                              // longest top-k by list
+constexpr int NUCLEUS = 128;                             // threads' maxima that a top-p's list begins from
 
 // An unsigned key in the order of the floats (-inf lowest; no NaN, and -0 is +0).
 __device__ __forceinline__ uint32_t key_of(float x) {
@@ -42,10 +52,20 @@ __device__ __forceinline__ u64 share(u64 W, u64 f) { return (W >> 31) * f + (((W
 // The row's scale of likelihoods.
 struct Scale {
     float top, slope;
-    __device__ __forceinline__ float octaves(float x) const { return __fmul_rn(x == top ? 0.0f : __fsub_rn(x, top), slope); }
-    __device__ __forceinline__ static u64 weight(float y) { return (u64)(__builtin_amdgcn_exp2f(y) * 0x1p40f); }
-    // (a logit of -inf has none, also where the slope is zero)
-    __device__ __forceinline__ u64 of(float x) const { return x == -INFINITY ? 0ull : weight(octaves(x)); }
+    // y of a logit that is no NaN.  (fminf: a difference of two infinities is no number, and stands for 0)
+    __device__ __forceinline__ float octaves(float x) const { return __fmul_rn(fminf(__fsub_rn(x, top), 0.0f), slope); }
+    __device__ __forceinline__ static float scaled(float y) { return __builtin_amdgcn_exp2f(y) * 0x1p40f; }     // 2^40 2^y
+    // its whole part, in two halves: 20 bits below, 21 above
+    __device__ __forceinline__ static void halves(float f, uint32_t &hi, uint32_t &lo) {
+        hi = (uint32_t)(f * 0x1p-20f);
+        lo = (uint32_t)__builtin_fmaf((float)hi, -0x1p20f, f);
+    }
+    __device__ __forceinline__ static u64 whole(float f) {
+        uint32_t hi, lo;
+        halves(f, hi, lo);
+        return ((u64)hi << 20) + lo;
+    }
+    __device__ __forceinline__ u64 of(float x) const { return whole(scaled(octaves(x))); }
 };
 
 __device__ __forceinline__ u64 wave_sum(u64 x) {
@@ -63,30 +83,87 @@ template <typename T> __device__ __forceinline__ T wave_before(T x, int lane) { 
     return s - x;
 }
 
-template <typename T> __device__ __forceinline__ float logit(const T *row, int i) {
-    const float x = to_f32(row[i]);
-    return x != x ? -INFINITY : x;
-}
-
-// f(logit, index) of every element, in steps that the whole workgroup takes together
-template <typename T, typename F> __device__ __forceinline__ void each(const T *row, int V, F &&f) {
-    for (int base = threadIdx.x * EACH; base < V; base += ROW_THREADS * EACH)
+// A row of logits from the 16-byte boundary at or before it: element v of the view is token v - off.
+template <typename T> struct Row {
+    const T *base;
+    int off, end;                                        // tokens are at off .. end - 1
+    __device__ __forceinline__ Row(const T *row, int V)
+        : base(reinterpret_cast<const T *>(reinterpret_cast<uintptr_t>(row) & ~(uintptr_t)15)), off((int)(row - base)), end(off + V) {}
+    struct Eight {
+        uint4 x[sizeof(T) == 2 ? 1 : 2];
+    };
+    // Elements v .. v + 7 (v a multiple of 8), and as numbers: -inf for a NaN and outside the row.
+    __device__ __forceinline__ Eight load(int v) const {
+        Eight e;
+        if (v >= off && v + EACH <= end) {
+            const uint4 *p = reinterpret_cast<const uint4 *>(base + v);
+            e.x[0] = p[0];
+            if constexpr (sizeof(T) == 4) e.x[1] = p[1];
+        } else {                                         // (nothing outside the row is read)
+            T t[EACH];
 #pragma unroll
-        for (int j = 0; j < EACH; ++j)
-            if (base + j < V) f(logit(row, base + j), base + j);
-}
+            for (int j = 0; j < EACH; ++j) t[j] = v + j >= off && v + j < end ? base[v + j] : from_f32<T>(-INFINITY);
+            __builtin_memcpy(&e, t, sizeof(e));
+        }
+        return e;
+    }
+    __device__ __forceinline__ static void numbers(const Eight &e, float *x) {
+        if constexpr (sizeof(T) == 2) {
+            const uint32_t w[4] = {e.x[0].x, e.x[0].y, e.x[0].z, e.x[0].w};
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                x[2 * j] = __builtin_bit_cast(float, w[j] << 16);
+                x[2 * j + 1] = __builtin_bit_cast(float, w[j] & 0xffff0000u);
+            }
+        } else {
+            __builtin_memcpy(x, &e, 32);
+        }
+#pragma unroll
+        for (int j = 0; j < EACH; ++j) x[j] = fmaxf(x[j], -INFINITY);
+    }
+    // f(eight numbers, their v) over the row, AT loads under way.  A wave's lanes take every step together (past the row's end
+    // with numbers of -inf).
+    template <typename F> __device__ __forceinline__ void each(F &&f) const {
+        constexpr int STEP = ROW_THREADS * EACH, AT = 2;
+        int first = (threadIdx.x & ~63) * EACH;
+        const int lane = (threadIdx.x & 63) * EACH;
+        for (; first + (AT - 1) * STEP < end; first += AT * STEP) {
+            Eight e[AT];
+#pragma unroll
+            for (int i = 0; i < AT; ++i) e[i] = load(first + lane + i * STEP);
+#pragma unroll
+            for (int i = 0; i < AT; ++i) {
+                float x[EACH];
+                numbers(e[i], x);
+                f(x, first + lane + i * STEP);
+            }
+        }
+        for (; first < end; first += STEP) {
+            float x[EACH];
+            numbers(load(first + lane), x);
+            f(x, first + lane);
+        }
+    }
+};
 
 struct Shared {
-    u64 weight[BINS];
-    uint32_t count[BINS];
-    u64 segment[MAX_V / SEGMENT];
-    uint32_t ties[MAX_V / SEGMENT];
-    u64 wave64[WAVES];
-    uint32_t wave32[WAVES];
+    union {
+        struct {                                         // a short list
+            u64 key[LIST];                               // logit's key above, ~index below: larger is earlier
+            u64 weight_at[LIST];                         // in order
+            uint32_t index_at[LIST];
+        } list;
+        struct {
+            u64 weight[BINS];
+            uint32_t count[BINS];
+            u64 segment[MAX_SEGMENTS];
+            uint32_t ties[MAX_SEGMENTS];
+        };
+    };
+    u64 wave64[WAVES], before64;
+    uint32_t wave32[WAVES], before32;
     float wavef[WAVES];
-    u64 before64;
-    uint32_t before32;
-    int at;
+    int at, listed;
 };
 
 // Where the running sum over `bins` bins (count or likelihood, from bin 0) reaches `need`: the bin, and both sums before it.
@@ -121,17 +198,45 @@ __device__ void clear(Shared &s, int bins) {
     __syncthreads();
 }
 
-template <typename T> __global__ __launch_bounds__(ROW_THREADS) void sample_kernel(SampleArgs a) {
+// The sum over the workgroup, and over the threads before this one.
+__device__ u64 group_sum(Shared &s, u64 x, u64 &before) {
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    before = wave_before(x, lane);
+    __syncthreads();
+    if (lane == 63) s.wave64[wave] = before + x;
+    __syncthreads();
+    u64 all = 0;
+    for (int w = 0; w < WAVES; ++w) {
+        const u64 y = s.wave64[w];
+        if (w < wave) before += y;
+        all += y;
+    }
+    return all;
+}
+
+// The point that u draws of a sum.
+__device__ __forceinline__ u64 drawn(u64 total, float u) { return share(total, (u64)(fminf(fmaxf(u, 0.0f), 1.0f - 0x1p-24f) * 0x1p31f)); }
+
+__device__ __forceinline__ void answer(const SampleArgs &a, int r, uint32_t token, const Scale &scale, float x, u64 total) {
+    a.token[r] = (int)token;
+    if (a.logprob) a.logprob[r] = scale.octaves(x) * 0.69314718055994530942f - logf((float)total * 0x1p-40f);
+}
+
+template <typename T> __global__ __launch_bounds__(ROW_THREADS, 8) void sample_kernel(SampleArgs a) {
     __shared__ Shared s;
     const int r = blockIdx.x, tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-    const T *row = (const T *)a.logits + (int64_t)r * a.row_stride;
-    const int V = a.V;
+    const Row<T> row((const T *)a.logits + (int64_t)r * a.row_stride, a.V);
 
-    float top = -INFINITY;
-    each(row, V, [&](float x, int) { top = fmaxf(top, x); });
+    float mine = -INFINITY;
+    row.each([&](const float *x, int) {
+#pragma unroll
+        for (int j = 0; j < EACH; ++j) mine = fmaxf(mine, x[j]);
+    });
+    float top = mine;
 #pragma unroll
     for (int d = 32; d > 0; d >>= 1) top = fmaxf(top, __shfl_xor(top, d));
     if (lane == 0) s.wavef[wave] = top;
+    if (tid == 0) s.listed = 0;
     __syncthreads();
     for (int w = 0; w < WAVES; ++w) top = fmaxf(top, s.wavef[w]);
     if (top == -INFINITY) {
@@ -145,7 +250,11 @@ template <typename T> __global__ __launch_bounds__(ROW_THREADS) void sample_kern
     const float temperature = a.temperature ? a.temperature[r] : 1.0f;
     if (!(temperature > 0.0f)) {                         // the first of the largest
         uint32_t first = 0xffffffffu;
-        each(row, V, [&](float x, int i) { first = x == top ? min(first, (uint32_t)i) : first; });
+        if (mine == top)
+            row.each([&](const float *x, int v) {
+#pragma unroll
+                for (int j = 0; j < EACH; ++j) first = x[j] == top ? min(first, (uint32_t)(v + j - row.off)) : first;
+            });
 #pragma unroll
         for (int d = 32; d > 0; d >>= 1) first = min(first, (uint32_t)__shfl_xor((int)first, d));
         if (lane == 0) s.wave32[wave] = first;
@@ -157,48 +266,135 @@ template <typename T> __global__ __launch_bounds__(ROW_THREADS) void sample_kern
         }
         return;
     }
-    const Scale scale{top, __fdiv_rn(1.44269504088896340736f, temperature)};
-    const float min_p = a.min_p ? a.min_p[r] : 0.0f, top_p = a.top_p ? a.top_p[r] : 1.0f;
-    const u64 least = min_p > 0.0f ? max((u64)(fminf(min_p, 1.0f) * 0x1p40f), 1ull) : 1ull;
+    // (an infinite temperature's slope is zero: tiny instead, so that a logit of -inf keeps no likelihood)
+    const Scale scale{top, fmaxf(__fdiv_rn(1.44269504088896340736f, temperature), 1e-37f)};
+    const float min_p = a.min_p ? a.min_p[r] : 0.0f, top_p = a.top_p ? a.top_p[r] : 1.0f, u = a.u[r];
+    // floor(w) >= least is w >= least: a whole number that fp32 holds
+    const float least = min_p > 0.0f ? fmaxf(floorf(fminf(min_p, 1.0f) * 0x1p40f), 1.0f) : 1.0f;
     const int top_k = a.top_k ? a.top_k[r] : 0;
-    const bool by_count = top_k > 0 && top_k < V, by_weight = top_p < 1.0f;
+    const bool by_count = top_k > 0 && top_k < a.V, by_weight = top_p < 1.0f;
+    const u64 part = (u64)(fmaxf(top_p, 0.0f) * 0x1p31f);            // top_p of a sum is share(sum, part); 0 where it is off
+
+    u64 all = 0;                                         // likelihoods of the whole row, where a top-p alone needs them
+    if ((by_count && top_k <= MOST_K) || (!by_count && by_weight)) {
+        // The bound: a value that `want` of the threads' maxima reach, and no other with its low 12 bits clear is larger.
+        const int want = by_count ? top_k : NUCLEUS;
+        const uint32_t mine_key = key_of(mine);
+        uint32_t t = 0;
+#pragma unroll 1
+        for (int bit = 31; bit >= 12; --bit)
+            if (__syncthreads_count(mine_key >= (t | 1u << bit)) >= want) t |= 1u << bit;
+        const float bound = t > key_of(-INFINITY) ? of_key(t) : -INFINITY;
+        auto list = [&](const float *x, int v) {
+#pragma unroll
+            for (int j = 0; j < EACH; ++j)
+                if (x[j] >= bound && x[j] > -INFINITY) {
+                    const int at = atomicAdd(&s.listed, 1);
+                    if (at < LIST) s.list.key[at] = (u64)key_of(x[j]) << 32 | (uint32_t)~(v + j - row.off);
+                }
+        };
+        if (by_count) {
+            if (mine >= bound) row.each(list);
+        } else {
+            row.each([&](const float *x, int v) {
+                uint32_t hi = 0, lo = 0;                 // (sums of eight halves of 21 and 20 bits)
+#pragma unroll
+                for (int j = 0; j < EACH; ++j) {
+                    const float f = Scale::scaled(scale.octaves(x[j]));
+                    uint32_t h, l;
+                    Scale::halves(f >= least ? f : 0.0f, h, l);
+                    hi += h;
+                    lo += l;
+                }
+                all += ((u64)hi << 20) + lo;
+                if (mine >= bound) list(x, v);
+            });
+            u64 before;
+            all = group_sum(s, all, before);
+        }
+        __syncthreads();
+        const int n = s.listed;
+        // Rank in the list, and the token in its place.
+        bool done = n <= LIST;
+        u64 w = 0, total = 0;
+        if (done) {
+            const u64 key = tid < n ? s.list.key[tid] : 0;
+            const float f = tid < n ? Scale::scaled(scale.octaves(of_key((uint32_t)(key >> 32)))) : 0.0f;
+            int at = 0;
+            if (tid < n) {
+                int t = 0;
+                for (; t + 1 < n; t += 2) {
+                    const ulonglong2 o = *reinterpret_cast<const ulonglong2 *>(&s.list.key[t]);
+                    at += (o.x > key) + (o.y > key);
+                }
+                if (t < n) at += s.list.key[t] > key;
+                s.list.weight_at[at] = f >= least && (!by_count || at < top_k) ? Scale::whole(f) : 0;
+                s.list.index_at[at] = ~(uint32_t)key;
+            }
+            __syncthreads();
+            w = tid < n ? s.list.weight_at[tid] : 0;
+            u64 before;
+            total = group_sum(s, w, before);
+            if (by_weight) {
+                const u64 need = max(share(by_count ? total : all, part), 1ull);
+                done = by_count || total >= need;        // (the same for every thread)
+                if (before >= need) w = 0;
+            }
+            if (done) {
+                if (by_weight) {
+                    s.list.weight_at[tid] = w;
+                    total = group_sum(s, w, before);     // (and a barrier: the weights are there)
+                }
+                const u64 point = drawn(total, u);
+                const uint32_t index = tid < n ? s.list.index_at[tid] : 0;
+                const int kept = __syncthreads_count(w > 0);          // a prefix
+                if (w > 0) {
+                    u64 sum = 0;                         // kept likelihoods before this token in the vocabulary
+                    for (int t = 0; t < kept; ++t) sum += s.list.index_at[t] < index ? s.list.weight_at[t] : 0;
+                    if (sum <= point && point < sum + w) {
+                        answer(a, r, index, scale, to_f32(row.base[row.off + index]), total);
+                    }
+                }
+                return;
+            }
+        }
+        __syncthreads();
+    }
 
     // Kept: keys above `cut`, and the first `ties` of those equal to it.
     uint32_t cut = 0, ties = 0xffffffffu;
     auto bin_of = [&](float y) { return min((int)(-y * BINS_PER_OCTAVE), BINS - 1); };
     if (by_count || by_weight) {
-        clear(s, BINS);
-        u64 all = 0;
-        uint32_t n = 0;
-        each(row, V, [&](float x, int) {
-            const u64 w = scale.of(x);
-            if (w < least) return;
-            const int i = bin_of(scale.octaves(x));
-            atomicAdd(&s.weight[i], w);
-            atomicAdd(&s.count[i], 1u);
-            all += w;
-            ++n;
-        });
-        all = wave_sum(all);
-        n = (uint32_t)wave_sum((u64)n);
-        if (lane == 0) s.wave64[wave] = all, s.wave32[wave] = n;
-        __syncthreads();
-        all = 0;
-        n = 0;
-        for (int w = 0; w < WAVES; ++w) all += s.wave64[w], n += s.wave32[w];
-
+        auto bins = [&](bool counted) {
+            clear(s, BINS);
+            row.each([&](const float *x, int) {
+#pragma unroll
+                for (int j = 0; j < EACH; ++j) {
+                    const float y = scale.octaves(x[j]), f = Scale::scaled(y);
+                    if (f < least) continue;
+                    const int i = bin_of(y);
+                    atomicAdd(&s.weight[i], Scale::whole(f));
+                    if (counted) atomicAdd(&s.count[i], 1u);
+                }
+            });
+        };
         // Inside bin `bin`: the key where the running sum reaches `need` (past what lies before the bin), and its ties.
         auto narrow = [&](int bin, bool weighs, u64 need, u64 &weight_before, uint32_t &count_before) {
             uint32_t prefix = 0, mask = 0;
             for (int shift = 24; shift >= (sizeof(T) == 2 ? 16 : 0); shift -= 8) {
                 clear(s, 256);
-                each(row, V, [&](float x, int) {
-                    const u64 w = scale.of(x);
-                    const uint32_t k = key_of(x);
-                    if (w < least || bin_of(scale.octaves(x)) != bin || (k & mask) != prefix) return;
-                    const int digit = 255 - (int)((k >> shift) & 255u);
-                    atomicAdd(&s.weight[digit], w);
-                    atomicAdd(&s.count[digit], 1u);
+                row.each([&](const float *x, int) {
+#pragma unroll
+                    for (int j = 0; j < EACH; ++j) {
+                        const float y = scale.octaves(x[j]);
+                        if (bin_of(y) != bin) continue;
+                        const uint32_t k = key_of(x[j]);
+                        const float f = Scale::scaled(y);
+                        if (f < least || (k & mask) != prefix) continue;
+                        const int digit = 255 - (int)((k >> shift) & 255u);
+                        atomicAdd(&s.weight[digit], Scale::whole(f));
+                        atomicAdd(&s.count[digit], 1u);
+                    }
                 });
                 int digit;
                 u64 wb;
@@ -215,51 +411,55 @@ template <typename T> __global__ __launch_bounds__(ROW_THREADS) void sample_kern
             const u64 w = scale.of(of_key(cut));
             ties = (uint32_t)(weighs ? (need + w - 1) / w : need);
         };
-        u64 kept = all;
+        auto sum_up = [&](u64 &w, uint32_t &c) {         // over all bins
+            __syncthreads();
+            w = 0;
+            c = 0;
+            for (int i = lane; i < BINS; i += 64) w += s.weight[i], c += s.count[i];
+            w = wave_sum(w);
+            c = (uint32_t)wave_sum((u64)c);
+        };
+        u64 kept;
+        uint32_t n;
+        bins(by_count);
+        sum_up(kept, n);
+        int bin;
+        u64 wb;
+        uint32_t cb;
         if (by_count && (uint32_t)top_k < n) {
-            int bin;
-            u64 wb;
-            uint32_t cb;
             find(s, BINS, false, top_k, bin, wb, cb);
             narrow(bin, false, (u64)top_k - cb, wb, cb);
             kept = wb + ties * scale.of(of_key(cut));
+            if (by_weight) bins(false);                  // (narrow wrote over them)
         }
         if (by_weight) {
-            const u64 need = max(share(kept, (u64)(fmaxf(top_p, 0.0f) * 0x1p31f)), 1ull);
-            clear(s, BINS);
-            each(row, V, [&](float x, int) {
-                const u64 w = scale.of(x);
-                if (w >= least) atomicAdd(&s.weight[bin_of(scale.octaves(x))], w);
-            });
-            int bin;
-            u64 wb;
-            uint32_t cb;
+            const u64 need = max(share(kept, part), 1ull);
             find(s, BINS, true, need, bin, wb, cb);
             narrow(bin, true, need - wb, wb, cb);
         }
     }
 
-    // Sums of what is kept, by segments of 512 tokens: above the cut, and how many ties.
-    const int segments = (V + SEGMENT - 1) / SEGMENT;
+    // Sums of what is kept, by segments of 512 elements: above the cut, and how many ties.
+    const int segments = (row.end + SEGMENT - 1) / SEGMENT;
     const u64 tie_weight = cut ? scale.of(of_key(cut)) : 0;
     __syncthreads();
-    for (int g = wave; g < segments; g += WAVES) {
-        u64 w = 0;
-        uint32_t t = 0;
+    row.each([&](const float *x, int v) {                // (a wave's step is a segment)
+        uint32_t hi = 0, lo = 0, t = 0;
+#pragma unroll
         for (int j = 0; j < EACH; ++j) {
-            const int i = g * SEGMENT + lane * EACH + j;
-            if (i >= V) break;
-            const float x = logit(row, i);
-            const u64 wx = scale.of(x);
-            const uint32_t k = key_of(x);
-            if (wx < least || k < cut) continue;
-            if (k == cut) ++t;
-            else w += wx;
+            const float f = Scale::scaled(scale.octaves(x[j]));
+            const uint32_t k = key_of(x[j]);
+            const bool ok = f >= least, tied = ok && k == cut;
+            uint32_t h, l;
+            Scale::halves(ok && k > cut ? f : 0.0f, h, l);
+            hi += h;
+            lo += l;
+            t += tied;
         }
-        w = wave_sum(w);
-        t = (uint32_t)wave_sum((u64)t);
-        if (lane == 0) s.segment[g] = w, s.ties[g] = t;
-    }
+        const u64 w = wave_sum(((u64)hi << 20) + lo);
+        if (cut) t = (uint32_t)wave_sum((u64)t);
+        if (lane == 0) s.segment[v / SEGMENT] = w, s.ties[v / SEGMENT] = t;
+    });
     __syncthreads();
     if (wave != 0) return;
 
@@ -272,32 +472,30 @@ template <typename T> __global__ __launch_bounds__(ROW_THREADS) void sample_kern
     u64 w = tied(tb, t);
     for (int i = 0; i < per; ++i) w += lane * per + i < segments ? s.segment[lane * per + i] : 0;
     u64 wb = wave_before(w, lane);
-    const u64 total = wave_sum(w);
-    const float u = a.u[r];
-    const u64 point = share(total, (u64)(fminf(fmaxf(u, 0.0f), 1.0f - 0x1p-24f) * 0x1p31f));
-    const bool mine = wb <= point && point < wb + w;
+    const u64 total = wave_sum(w), point = drawn(total, u);
+    const bool here = wb <= point && point < wb + w;
     int g = lane * per;
-    if (mine) {
+    if (here) {
         for (;; ++g) {
-            const u64 here = s.segment[g] + tied(tb, s.ties[g]);
-            if (point < wb + here) break;
-            wb += here;
+            const u64 more = s.segment[g] + tied(tb, s.ties[g]);
+            if (point < wb + more) break;
+            wb += more;
             tb += s.ties[g];
         }
     }
-    const int from = __builtin_ctzll(__ballot(mine));    // (point is below the total: one lane has it)
+    const int from = __builtin_ctzll(__ballot(here));    // (point is below the total: one lane has it)
     g = __shfl(g, from);
     wb = __shfl(wb, from);
     tb = __shfl(tb, from);
     float x[EACH];
     u64 wx[EACH];
+    const int v = g * SEGMENT + lane * EACH;
+    Row<T>::numbers(row.load(v), x);
     t = 0;
 #pragma unroll
     for (int j = 0; j < EACH; ++j) {
-        const int i = g * SEGMENT + lane * EACH + j;
-        x[j] = i < V ? logit(row, i) : -INFINITY;
-        wx[j] = scale.of(x[j]);
-        if (wx[j] < least || key_of(x[j]) < cut) wx[j] = 0;
+        const float f = Scale::scaled(scale.octaves(x[j]));
+        wx[j] = f >= least && key_of(x[j]) >= cut ? Scale::whole(f) : 0;
         t += wx[j] && key_of(x[j]) == cut;
     }
     tb += wave_before(t, lane);
@@ -311,10 +509,7 @@ template <typename T> __global__ __launch_bounds__(ROW_THREADS) void sample_kern
     if (wb <= point && point < wb + w) {
 #pragma unroll
         for (int j = 0; j < EACH; ++j) {
-            if (wb <= point && point < wb + wx[j]) {
-                a.token[r] = g * SEGMENT + lane * EACH + j;
-                if (a.logprob) a.logprob[r] = scale.octaves(x[j]) * 0.69314718055994530942f - logf((float)total * 0x1p-40f);
-            }
+            if (wb <= point && point < wb + wx[j]) answer(a, r, (uint32_t)(v + j - row.off), scale, x[j], total);
             wb += wx[j];
         }
     }
