@@ -845,20 +845,21 @@ template <typename S> __global__ __launch_bounds__(S::NT, S::OCCUPANCY) void att
     }
 }
 
-// Joins the parts of the units that were cut: a workgroup per (unit, 32 rows, 32 values), its waves sharing the parts.
-template <typename S> __global__ __launch_bounds__(256) void join_kernel(Work w) {
+// Joins the parts of the units that were cut.  MANY: a workgroup per (unit, 32 rows), its four waves take every fourth 32 values;
+// otherwise a workgroup per (unit, 32 rows, 32 values), whose waves take every fourth part (few units may have many parts).
+template <typename S, bool MANY> __global__ __launch_bounds__(256) void join_kernel(Work w) {
     constexpr int KT = S::KT, RT = S::RT, DT = S::DT;
     using T = typename S::T;
-    __shared__ float sums[4][17][64], tops[4][64];
+    __shared__ float sums[MANY ? 1 : 4][17][64], tops[4][64];
     const AttendArgs &a = w.a;
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, hg = lane >> 5;
-    const int dt = blockIdx.x % DT, wr = blockIdx.x / DT % S::WR, unit = blockIdx.x / (DT * S::WR);
+    const int lane = threadIdx.x & 63, wave = uniform(threadIdx.x >> 6), hg = lane >> 5;
+    const int at_unit = MANY ? blockIdx.x : blockIdx.x / DT, wr = at_unit % S::WR, unit = at_unit / S::WR;
     const int b = unit / (a.H_kv * w.c.units), n = unit - b * a.H_kv * w.c.units, h = n / w.c.units, rt = n - h * w.c.units;
     const int r = rt * RT + wr * 32 + (lane & 31);
     if (rt * RT + wr * 32 >= w.c.M) return;
-    const int64_t total = w.p.first[a.B];
+    const int64_t total = w.p.first[a.B], before = w.p.first[b];
     const int groups = w.p.info[0], old = own_tiles(a, KT, cached(a, b));
-    int64_t begin = w.p.first[b] + (int64_t)h * (w.c.units * old + w.c.draft_tiles);
+    int64_t begin = before + (int64_t)h * (w.c.units * old + w.c.draft_tiles);
     for (int i = 0; i < rt; ++i) begin += old + draft_tiles_of(i, RT, KT, w.c.G, a.N);
     const int64_t end = begin + old + draft_tiles_of(rt, RT, KT, w.c.G, a.N);
     const int64_t shared_ids = (int64_t)a.H_kv * w.c.shared_units;
@@ -884,43 +885,51 @@ template <typename S> __global__ __launch_bounds__(256) void join_kernel(Work w)
         span[1].lane = (int)(row % RT);
     }
     auto slot = [&](const Span &x, int i) { return slot_of(w.c.groups, x.unit, i == 0, i == x.count - 1, x.first + i); };
+    const int from_part = MANY ? 0 : wave, parts_step = MANY ? 1 : 4;
     float top = -INFINITY;
     if (live)
         for (int k = 0; k < 2; ++k)
-            for (int i = wave; i < span[k].count; i += 4) top = fmaxf(top, w.ml[slot(span[k], i) * RT + span[k].lane].x);
-    tops[wave][lane] = top;
-    __syncthreads();
-    for (int i = 0; i < 4; ++i) top = fmaxf(top, tops[i][lane]);
-    float sum = 0.0f, x[16] = {};
-    if (live)
-        for (int k = 0; k < 2; ++k)
-            for (int i = wave; i < span[k].count; i += 4) {
-                const int64_t at = slot(span[k], i);
-                const float2 ml = w.ml[at * RT + span[k].lane];
-                const float by = ml.x == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(ml.x - top);
-                sum += by * ml.y;
-                const float *from = w.part + ((at * S::WR + span[k].lane / 32) * DT + dt) * 1024 + (hg * 32 + span[k].lane % 32) * 4;
-#pragma unroll
-                for (int j = 0; j < 4; ++j) {
-                    const f32x4 y = *reinterpret_cast<const f32x4 *>(from + j * 256);
-#pragma unroll
-                    for (int r = 0; r < 4; ++r) x[4 * j + r] += by * y[r];
-                }
-            }
-#pragma unroll
-    for (int j = 0; j < 16; ++j) sums[wave][j][lane] = x[j];
-    sums[wave][16][lane] = sum;
-    __syncthreads();
-    if (wave != 0 || !live) return;
-    f32x16 o;
-    for (int i = 1; i < 4; ++i) sum += sums[i][16][lane];
-#pragma unroll
-    for (int j = 0; j < 16; ++j) {
-        o[j] = x[j];
-        for (int i = 1; i < 4; ++i) o[j] += sums[i][j][lane];
+            for (int i = from_part; i < span[k].count; i += parts_step) top = fmaxf(top, w.ml[slot(span[k], i) * RT + span[k].lane].x);
+    if constexpr (!MANY) {
+        tops[wave][lane] = top;
+        __syncthreads();
+        for (int i = 0; i < 4; ++i) top = fmaxf(top, tops[i][lane]);
     }
     const int node = r / w.c.G;
-    store_row<T>(out_row<T>(a, b, h * w.c.G + r - node * w.c.G, node), dt, hg, o, 1.0f / sum);
+    T *out = live ? out_row<T>(a, b, h * w.c.G + r - node * w.c.G, node) : nullptr;
+    for (int dt = MANY ? wave : blockIdx.x % DT; dt < DT; dt += MANY ? 4 : DT) {
+        float sum = 0.0f;
+        f32x4 x[4] = {};
+        if (live)
+            for (int k = 0; k < 2; ++k)
+                for (int i = from_part; i < span[k].count; i += parts_step) {
+                    const int64_t at = slot(span[k], i);
+                    const float2 ml = w.ml[at * RT + span[k].lane];
+                    const float *from = w.part + ((at * S::WR + span[k].lane / 32) * DT + dt) * 1024 + (hg * 32 + span[k].lane % 32) * 4;
+                    f32x4 y[4];
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) y[j] = *reinterpret_cast<const f32x4 *>(from + j * 256);
+                    const float by = ml.x == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(ml.x - top);
+                    sum += by * ml.y;
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) x[j] += by * y[j];
+                }
+        f32x16 o;
+#pragma unroll
+        for (int j = 0; j < 16; ++j) o[j] = x[j / 4][j % 4];
+        if constexpr (!MANY) {
+#pragma unroll
+            for (int j = 0; j < 16; ++j) sums[wave][j][lane] = o[j];
+            sums[wave][16][lane] = sum;
+            __syncthreads();
+            if (wave != 0) return;
+            for (int i = 1; i < 4; ++i) sum += sums[i][16][lane];
+#pragma unroll
+            for (int j = 0; j < 16; ++j)
+                for (int i = 1; i < 4; ++i) o[j] += sums[i][j][lane];
+        }
+        if (live) store_row<T>(out, dt, hg, o, 1.0f / sum);
+    }
 }
 
 // ---- host ----------------------------------------------------------------------
@@ -984,8 +993,11 @@ template <typename S> hipError_t run(const AttendArgs &a, void *workspace, hipSt
     hipLaunchKernelGGL((prepare_kernel<typename S::T, S::HD>), dim3((unsigned)(a.B * w.prep_blocks + 1)), dim3(THREADS), 0, stream, w,
                        S::RT, S::KT);
     hipLaunchKernelGGL((attend_kernel<S>), dim3((unsigned)(w.c.groups ? w.c.groups : units)), dim3(S::NT), 0, stream, w);
-    if (w.c.groups)
-        hipLaunchKernelGGL((join_kernel<S>), dim3((unsigned)(units * S::WR * S::DT)), dim3(256), 0, stream, w);
+    // (the first form from as many workgroups as fill the device; 16 x 8-node chains, 16 parts each, took 7.6 us by the second)
+    if (w.c.groups && units * S::WR >= 2 * compute_units())
+        hipLaunchKernelGGL((join_kernel<S, true>), dim3((unsigned)(units * S::WR)), dim3(256), 0, stream, w);
+    else if (w.c.groups)
+        hipLaunchKernelGGL((join_kernel<S, false>), dim3((unsigned)(units * S::WR * S::DT)), dim3(256), 0, stream, w);
     return hipGetLastError();
 }
 
