@@ -126,8 +126,15 @@ template <typename A> __device__ __forceinline__ int cached(const A &a, int b) {
 __device__ __forceinline__ int own_tiles(const AttendArgs &a, int KT, int len) { return (max(len - a.shared, 0) + KT - 1) / KT; }
 
 // Workgroup whose part holds tile x, and the first tile of workgroup g.
-__device__ __forceinline__ int64_t first_of(int64_t total, int groups, int64_t g) { return total * g / groups; }
-__device__ __forceinline__ int group_of(int64_t total, int groups, int64_t x) { return (int)(((x + 1) * groups - 1) / total); }
+// (in 32 bits where they hold it: a 64-bit division is some 150 instructions)
+__device__ __forceinline__ int64_t first_of(int64_t total, int groups, int64_t g) {
+    if (total < (1 << 21) && groups < (1 << 10)) return (uint32_t)total * (uint32_t)g / (uint32_t)groups;
+    return total * g / groups;
+}
+__device__ __forceinline__ int group_of(int64_t total, int groups, int64_t x) {
+    if (total < (1 << 21) && groups < (1 << 10)) return (int)((((uint32_t)x + 1) * (uint32_t)groups - 1) / (uint32_t)total);
+    return (int)(((x + 1) * groups - 1) / total);
+}
 
 // Where group g puts its part of the unit with tiles [begin, end): a group has at most one part that does not begin its unit,
 // and one that begins it and does not end it.
@@ -163,10 +170,11 @@ template <typename T> __device__ __forceinline__ uint4 finite(uint4 x) {
 
 // The list: first tiles, and where every group begins.  One workgroup.
 __device__ void make_list(const Work &w, int RT, int KT) {
-    __shared__ int64_t sums[THREADS];
-    __shared__ int most[THREADS], who[THREADS];
+    constexpr int WAVES = THREADS / 64;
+    __shared__ int64_t sums[WAVES];
+    __shared__ int most[WAVES], who[WAVES];
     const AttendArgs &a = w.a;
-    const int tid = threadIdx.x, per = (a.B + THREADS - 1) / THREADS;
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, per = (a.B + THREADS - 1) / THREADS;
     const int64_t shared = (int64_t)a.H_kv * w.c.shared_units * w.c.shared_tiles;
     auto tiles_of = [&](int b) {
         return (int64_t)a.H_kv * ((int64_t)w.c.units * own_tiles(a, KT, cached(a, b)) + w.c.draft_tiles);
@@ -178,20 +186,22 @@ __device__ void make_list(const Work &w, int RT, int KT) {
         sum += tiles_of(b);
         if (len > top) top = len, at = b;
     }
-    sums[tid] = sum;
-    most[tid] = top;
-    who[tid] = at;
-    for (int d = 1; d < THREADS; d <<= 1) {
-        __syncthreads();
-        const int64_t x = tid >= d ? sums[tid - d] : 0;
-        const int m = tid >= d ? most[tid - d] : -1, o = tid >= d ? who[tid - d] : 0;
-        __syncthreads();
-        sums[tid] += x;
-        if (m >= most[tid]) most[tid] = m, who[tid] = o;
+    int64_t before = sum;
+#pragma unroll
+    for (int d = 1; d < 64; d <<= 1) {
+        const int64_t x = __shfl_up(before, d);
+        const int m = __shfl_xor(top, d), o = __shfl_xor(at, d);
+        if (lane >= d) before += x;
+        if (m > top || (m == top && o < at)) top = m, at = o;
     }
+    if (lane == 63) sums[wave] = before, most[wave] = top, who[wave] = at;
     __syncthreads();
-    const int64_t total = shared + sums[THREADS - 1];
-    int64_t next = shared + sums[tid] - sum;
+    int64_t total = shared, next = shared + before - sum;
+    for (int i = 0; i < WAVES; ++i) {
+        if (i < wave) next += sums[i];
+        total += sums[i];
+        if (most[i] > top || (most[i] == top && who[i] < at)) top = most[i], at = who[i];
+    }
     for (int b = tid * per; b < min(a.B, (tid + 1) * per); ++b) {
         w.p.first[b] = next;
         next += tiles_of(b);
@@ -213,7 +223,7 @@ __device__ void make_list(const Work &w, int RT, int KT) {
         }
         const int64_t x = first_of(total, groups, g);
         s.group = g;
-        s.longest = who[THREADS - 1];
+        s.longest = at;
         s.tiles = (int)(first_of(total, groups, g + 1) - x);
         if (x < shared) {
             const int n = (int)(x / w.c.shared_tiles);
@@ -1016,7 +1026,7 @@ template <typename F> auto choose(int rows, int d, int rot, bool f32, F &&f) {
     }
     if (d == 128) {
         if (rows <= 32) return f(Shape<__bf16, 128, 1, 4, 128, 8>{});
-        if (rows <= 64) return f(Shape<__bf16, 128, 2, 2, 128, 8>{});
+        if (rows <= 64) return f(Shape<__bf16, 128, 2, 2, 64, 8>{});
         return rows <= 128 ? f(Shape<__bf16, 128, 4, 1, 64, 8>{}) : f(Shape<__bf16, 128, 8, 1, 128, 8>{});
     }
     if (rot <= 64) {
