@@ -13,11 +13,12 @@
 //    row as well, where the list proves to hold enough).
 //  - Where that does not do (a flat row's top-p, thousands of ties), a pass
 //    counts tokens and likelihoods by bins of 1/12 octave below the largest,
-//    which shows the bin that the prefix ends in, passes over the digits of
-//    that bin's logits narrow it to one logit `cut` and a number of its ties,
-//    and a last pass sums what is kept by segments of the vocabulary.  The
-//    segment that holds the drawn point is walked by one wave.  Without top-k
-//    and top-p only this last pass is needed.
+//    which shows the bin that the prefix ends in, and passes over the keys
+//    below that bin's largest (one for bf16 but near zero) narrow it to one
+//    logit `cut` and a number of its ties.
+//  - A last pass sums what is kept by sixteen parts of the vocabulary; the wave
+//    that the drawn point falls to walks its part.  Without top-k and top-p this
+//    pass and the first are all.
 #include "hybrid_launch.h"
 #include "device.h"
 
@@ -29,8 +30,7 @@ typedef unsigned long long u64;
 
 constexpr int ROW_THREADS = 1024, WAVES = ROW_THREADS / 64;
 constexpr int EACH = 8;                                  // elements of a thread in one step
-constexpr int SEGMENT = 64 * EACH;                       // ... of a wave: one segment of the last pass
-constexpr int MAX_V = 1 << 20, MAX_SEGMENTS = MAX_V / SEGMENT + 1;
+constexpr int STEP = 64 * EACH;                          // ... of a wave
 constexpr int BINS = 512;                                // 1/12 octave each; 2^-40 is in bin 480
 constexpr float BINS_PER_OCTAVE = 12.0f;
 constexpr int LIST = ROW_THREADS;                        // longest list: a thread per token
@@ -67,6 +67,9 @@ struct Scale {
     }
     __device__ __forceinline__ u64 of(float x) const { return whole(scaled(octaves(x))); }
 };
+
+// Sums of up to 2^13 likelihoods are exact in a double (three instructions each, where whole numbers of 64 bits take seven).
+__device__ __forceinline__ double exactly(float f) { return (double)floorf(f); }
 
 __device__ __forceinline__ u64 wave_sum(u64 x) {
 #pragma unroll
@@ -121,28 +124,30 @@ template <typename T> struct Row {
 #pragma unroll
         for (int j = 0; j < EACH; ++j) x[j] = fmaxf(x[j], -INFINITY);
     }
-    // f(eight numbers, their v) over the row, AT loads under way.  A wave's lanes take every step together (past the row's end
-    // with numbers of -inf).
-    template <typename F> __device__ __forceinline__ void each(F &&f) const {
-        constexpr int STEP = ROW_THREADS * EACH, AT = 2;
-        int first = (threadIdx.x & ~63) * EACH;
+    // f(eight numbers, their v) over first, first + step, ... below `last`, AT loads under way.  A wave's lanes take every step
+    // together (past the row's end with numbers of -inf).
+    template <typename F> __device__ __forceinline__ void walk(int first, int step, int last, F &&f) const {
+        constexpr int AT = 2;
         const int lane = (threadIdx.x & 63) * EACH;
-        for (; first + (AT - 1) * STEP < end; first += AT * STEP) {
+        for (; first + (AT - 1) * step < last; first += AT * step) {
             Eight e[AT];
 #pragma unroll
-            for (int i = 0; i < AT; ++i) e[i] = load(first + lane + i * STEP);
+            for (int i = 0; i < AT; ++i) e[i] = load(first + lane + i * step);
 #pragma unroll
             for (int i = 0; i < AT; ++i) {
                 float x[EACH];
                 numbers(e[i], x);
-                f(x, first + lane + i * STEP);
+                f(x, first + lane + i * step);
             }
         }
-        for (; first < end; first += STEP) {
+        for (; first < last; first += step) {
             float x[EACH];
             numbers(load(first + lane), x);
             f(x, first + lane);
         }
+    }
+    template <typename F> __device__ __forceinline__ void each(F &&f) const {
+        walk((threadIdx.x & ~63) * EACH, ROW_THREADS * EACH, end, f);
     }
 };
 
@@ -156,8 +161,6 @@ struct Shared {
         struct {
             u64 weight[BINS];
             uint32_t count[BINS];
-            u64 segment[MAX_SEGMENTS];
-            uint32_t ties[MAX_SEGMENTS];
         };
     };
     u64 wave64[WAVES], before64;
@@ -296,21 +299,17 @@ template <typename T> __global__ __launch_bounds__(ROW_THREADS, 8) void sample_k
         if (by_count) {
             if (mine >= bound) row.each(list);
         } else {
+            double sum = 0.0;
             row.each([&](const float *x, int v) {
-                uint32_t hi = 0, lo = 0;                 // (sums of eight halves of 21 and 20 bits)
 #pragma unroll
                 for (int j = 0; j < EACH; ++j) {
                     const float f = Scale::scaled(scale.octaves(x[j]));
-                    uint32_t h, l;
-                    Scale::halves(f >= least ? f : 0.0f, h, l);
-                    hi += h;
-                    lo += l;
+                    sum += exactly(f >= least ? f : 0.0f);
                 }
-                all += ((u64)hi << 20) + lo;
                 if (mine >= bound) list(x, v);
             });
             u64 before;
-            all = group_sum(s, all, before);
+            all = group_sum(s, (u64)sum, before);
         }
         __syncthreads();
         const int n = s.listed;
@@ -378,36 +377,47 @@ template <typename T> __global__ __launch_bounds__(ROW_THREADS, 8) void sample_k
                 }
             });
         };
-        // Inside bin `bin`: the key where the running sum reaches `need` (past what lies before the bin), and its ties.
+        // From bin `bin` on: the key where the running sum reaches `need` (past what lies before the bin), and its ties.  Keys
+        // (a bf16's upper half) are counted by their distance from the largest that is left, in steps that 512 bins hold.
         auto narrow = [&](int bin, bool weighs, u64 need, u64 &weight_before, uint32_t &count_before) {
-            uint32_t prefix = 0, mask = 0;
-            for (int shift = 24; shift >= (sizeof(T) == 2 ? 16 : 0); shift -= 8) {
-                clear(s, 256);
+            constexpr int LOW = sizeof(T) == 2 ? 16 : 0;
+            auto number = [](uint32_t k) { return of_key(LOW && !(k >> 15) ? k << LOW | 0xffffu : k << LOW); };
+            auto bounded = [&](int at_least) {           // the largest key that is in bin `at_least` or after it
+                uint32_t k = 0;
+                for (int bit = 31 - LOW; bit >= 0; --bit)
+                    if (number(k | 1u << bit) <= top && bin_of(scale.octaves(number(k | 1u << bit))) >= at_least) k |= 1u << bit;
+                return k;
+            };
+            uint32_t last = bounded(bin), range = last - bounded(bin + 1);          // keys last, last - 1, ... of the bin
+            for (bool found = false; !found;) {
+                const int shift = max(0, 32 - __builtin_clz(range | 1) - 9);        // (range >> shift is below 512)
+                clear(s, BINS);
                 row.each([&](const float *x, int) {
 #pragma unroll
                     for (int j = 0; j < EACH; ++j) {
-                        const float y = scale.octaves(x[j]);
-                        if (bin_of(y) != bin) continue;
-                        const uint32_t k = key_of(x[j]);
-                        const float f = Scale::scaled(y);
-                        if (f < least || (k & mask) != prefix) continue;
-                        const int digit = 255 - (int)((k >> shift) & 255u);
-                        atomicAdd(&s.weight[digit], Scale::whole(f));
-                        atomicAdd(&s.count[digit], 1u);
+                        const uint32_t k = key_of(x[j]) >> LOW, at = (last - k) >> shift;
+                        if (k > last || at >= (uint32_t)BINS) continue;
+                        const float f = Scale::scaled(scale.octaves(x[j]));
+                        if (f < least) continue;
+                        if (weighs) atomicAdd(&s.weight[at], Scale::whole(f));
+                        else {
+                            atomicAdd(&s.weight[at], Scale::whole(f));
+                            atomicAdd(&s.count[at], 1u);
+                        }
                     }
                 });
-                int digit;
+                int at;
                 u64 wb;
                 uint32_t cb;
-                find(s, 256, weighs, need, digit, wb, cb);
+                find(s, BINS, weighs, need, at, wb, cb);
                 need -= weighs ? wb : (u64)cb;
                 weight_before += wb;
                 count_before += cb;
-                prefix |= (uint32_t)(255 - digit) << shift;
-                mask |= 255u << shift;
+                last -= (uint32_t)at << shift;
+                range = 1u << shift;
+                found = shift == 0;
             }
-            // (a bf16's low half: zeros above zero, ones below)
-            cut = sizeof(T) == 2 && !(prefix & 0x80000000u) ? prefix | 0xffffu : prefix;
+            cut = key_of(number(last));
             const u64 w = scale.of(of_key(cut));
             ties = (uint32_t)(weighs ? (need + w - 1) / w : need);
         };
@@ -439,79 +449,63 @@ template <typename T> __global__ __launch_bounds__(ROW_THREADS, 8) void sample_k
         }
     }
 
-    // Sums of what is kept, by segments of 512 elements: above the cut, and how many ties.
-    const int segments = (row.end + SEGMENT - 1) / SEGMENT;
+    // Sums of what is kept, by the waves' parts of the row: above the cut, and how many ties.
+    const int share_of = (row.end + WAVES * STEP - 1) / (WAVES * STEP) * STEP, first = wave * share_of, last = min(row.end, first + share_of);
     const u64 tie_weight = cut ? scale.of(of_key(cut)) : 0;
-    __syncthreads();
-    row.each([&](const float *x, int v) {                // (a wave's step is a segment)
-        uint32_t hi = 0, lo = 0, t = 0;
+    const float cut_at = cut ? of_key(cut) : -INFINITY;  // (a row's logits with likelihoods are above it, or it)
+    auto sums = [&](const float *x, double &w, uint32_t &t) {
 #pragma unroll
         for (int j = 0; j < EACH; ++j) {
             const float f = Scale::scaled(scale.octaves(x[j]));
-            const uint32_t k = key_of(x[j]);
-            const bool ok = f >= least, tied = ok && k == cut;
-            uint32_t h, l;
-            Scale::halves(ok && k > cut ? f : 0.0f, h, l);
-            hi += h;
-            lo += l;
-            t += tied;
+            w += exactly(f >= least && x[j] > cut_at ? f : 0.0f);
+            t += f >= least && x[j] == cut_at;
         }
-        const u64 w = wave_sum(((u64)hi << 20) + lo);
-        if (cut) t = (uint32_t)wave_sum((u64)t);
-        if (lane == 0) s.segment[v / SEGMENT] = w, s.ties[v / SEGMENT] = t;
-    });
-    __syncthreads();
-    if (wave != 0) return;
-
-    // The first wave: the segment that the drawn point lies in, then its tokens.
-    auto tied = [&](uint32_t before, uint32_t here) { return tie_weight * (min(ties, before + here) - min(ties, before)); };
-    const int per = (segments + 63) / 64;
+    };
+    double w = 0.0;
     uint32_t t = 0;
-    for (int i = 0; i < per; ++i) t += lane * per + i < segments ? s.ties[lane * per + i] : 0;
-    uint32_t tb = wave_before(t, lane);
-    u64 w = tied(tb, t);
-    for (int i = 0; i < per; ++i) w += lane * per + i < segments ? s.segment[lane * per + i] : 0;
-    u64 wb = wave_before(w, lane);
-    const u64 total = wave_sum(w), point = drawn(total, u);
-    const bool here = wb <= point && point < wb + w;
-    int g = lane * per;
-    if (here) {
-        for (;; ++g) {
-            const u64 more = s.segment[g] + tied(tb, s.ties[g]);
-            if (point < wb + more) break;
-            wb += more;
-            tb += s.ties[g];
+    row.walk(first, STEP, last, [&](const float *x, int) { sums(x, w, t); });
+    u64 mine64 = wave_sum((u64)w);
+    t = (uint32_t)wave_sum((u64)t);
+    __syncthreads();
+    if (lane == 0) s.wave64[wave] = mine64, s.wave32[wave] = t;
+    __syncthreads();
+    // The wave whose part the drawn point falls to, and what lies before it.
+    auto tied = [&](uint32_t before, uint32_t here) { return tie_weight * (min(ties, before + here) - min(ties, before)); };
+    u64 total = 0, wb = 0;
+    uint32_t tb = 0, passed = 0;
+    for (int i = 0; i < WAVES; ++i) {
+        const uint32_t ti = s.wave32[i];
+        const u64 wi = s.wave64[i] + tied(passed, ti);
+        if (i < wave) wb += wi, tb += ti;
+        total += wi;
+        passed += ti;
+    }
+    const u64 point = drawn(total, u);
+    if (point < wb || point >= wb + mine64 + tied(tb, t)) return;
+    // Its steps, then the eight tokens of a lane.
+    for (int base = first; base < last; base += STEP) {
+        const int v = base + lane * EACH;
+        float x[EACH];
+        Row<T>::numbers(row.load(v), x);
+        w = 0.0;
+        t = 0;
+        sums(x, w, t);
+        uint32_t tl = tb + wave_before(t, lane);
+        u64 wl = (u64)w + tied(tl, t), before = wb + wave_before(wl, lane);
+        const bool here = point >= before && point < before + wl;
+        if (here) {
+#pragma unroll
+            for (int j = 0; j < EACH; ++j) {
+                const float f = Scale::scaled(scale.octaves(x[j]));
+                const bool tie = f >= least && x[j] == cut_at;
+                const u64 wx = tie ? (tl++ < ties ? tie_weight : 0) : f >= least && x[j] > cut_at ? Scale::whole(f) : 0;
+                if (point >= before && point < before + wx) answer(a, r, (uint32_t)(v + j - row.off), scale, x[j], total);
+                before += wx;
+            }
         }
-    }
-    const int from = __builtin_ctzll(__ballot(here));    // (point is below the total: one lane has it)
-    g = __shfl(g, from);
-    wb = __shfl(wb, from);
-    tb = __shfl(tb, from);
-    float x[EACH];
-    u64 wx[EACH];
-    const int v = g * SEGMENT + lane * EACH;
-    Row<T>::numbers(row.load(v), x);
-    t = 0;
-#pragma unroll
-    for (int j = 0; j < EACH; ++j) {
-        const float f = Scale::scaled(scale.octaves(x[j]));
-        wx[j] = f >= least && key_of(x[j]) >= cut ? Scale::whole(f) : 0;
-        t += wx[j] && key_of(x[j]) == cut;
-    }
-    tb += wave_before(t, lane);
-    w = 0;
-#pragma unroll
-    for (int j = 0; j < EACH; ++j) {
-        if (wx[j] && key_of(x[j]) == cut && tb++ >= ties) wx[j] = 0;
-        w += wx[j];
-    }
-    wb += wave_before(w, lane);
-    if (wb <= point && point < wb + w) {
-#pragma unroll
-        for (int j = 0; j < EACH; ++j) {
-            if (wb <= point && point < wb + wx[j]) answer(a, r, (uint32_t)(v + j - row.off), scale, x[j], total);
-            wb += wx[j];
-        }
+        if (__any(here)) return;
+        wb += wave_sum(wl);
+        tb += (uint32_t)wave_sum((u64)t);
     }
 }
 
