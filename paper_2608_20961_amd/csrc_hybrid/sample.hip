@@ -7,9 +7,9 @@
 // A workgroup has a row.  The tokens that the filters keep are a prefix of the
 // order (logit down, index up), which is never sorted as a whole:
 //  - The first pass finds the largest logit, of the row and of each thread's
-//    share.  The k-th largest of the 1024 threads' is a bound that at least k
-//    tokens reach, and few more do: the second pass lists those, and all else
-//    is done on the list (top-k up to 512; top-p, whose second pass sums the
+//    share.  The k-th largest of 512 pairs of threads' is a bound that at least
+//    k tokens reach, and few more do: the second pass lists those, and all else
+//    is done on the list (top-k up to 256; top-p, whose second pass sums the
 //    row as well, where the list proves to hold enough).
 //  - Where that does not do (a flat row's top-p, thousands of ties), a pass
 //    counts tokens and likelihoods by bins of 1/12 octave below the largest,
@@ -34,7 +34,8 @@ constexpr int STEP = 64 * EACH;                          // ... of a wave
 constexpr int BINS = 512;                                // 1/12 octave each; 2^-40 is in bin 480
 constexpr float BINS_PER_OCTAVE = 12.0f;
 constexpr int LIST = ROW_THREADS;                        // longest list: a thread per token
-constexpr int MOST_K = 512;                              // longest top-k by list
+constexpr int PAIRS = ROW_THREADS / 2;
+constexpr int MOST_K = 256;                              // longest top-k by list
 constexpr int NUCLEUS = 128;                             // threads' maxima that a top-p's list begins from
 
 // An unsigned key in the order of the floats (-inf lowest; no NaN, and -0 is +0).
@@ -124,9 +125,9 @@ template <typename T> struct Row {
 #pragma unroll
         for (int j = 0; j < EACH; ++j) x[j] = fmaxf(x[j], -INFINITY);
     }
-    // f(eight numbers, their v) over first, first + step, ... below `last`, AT loads under way.  A wave's lanes take every step
-    // together (past the row's end with numbers of -inf).
-    template <typename F> __device__ __forceinline__ void walk(int first, int step, int last, F &&f) const {
+    // f(eight elements, their v) over first, first + step, ... below `last`, AT loads under way.  A wave's lanes take every step
+    // together (past the row's end with elements of -inf).
+    template <typename F> __device__ __forceinline__ void raw(int first, int step, int last, F &&f) const {
         constexpr int AT = 2;
         const int lane = (threadIdx.x & 63) * EACH;
         for (; first + (AT - 1) * step < last; first += AT * step) {
@@ -134,22 +135,56 @@ template <typename T> struct Row {
 #pragma unroll
             for (int i = 0; i < AT; ++i) e[i] = load(first + lane + i * step);
 #pragma unroll
-            for (int i = 0; i < AT; ++i) {
-                float x[EACH];
-                numbers(e[i], x);
-                f(x, first + lane + i * step);
-            }
+            for (int i = 0; i < AT; ++i) f(e[i], first + lane + i * step);
         }
-        for (; first < last; first += step) {
+        for (; first < last; first += step) f(load(first + lane), first + lane);
+    }
+    template <typename F> __device__ __forceinline__ void walk(int first, int step, int last, F &&f) const {
+        raw(first, step, last, [&](const Eight &e, int v) {
             float x[EACH];
-            numbers(load(first + lane), x);
-            f(x, first + lane);
-        }
+            numbers(e, x);
+            f(x, v);
+        });
     }
     template <typename F> __device__ __forceinline__ void each(F &&f) const {
         walk((threadIdx.x & ~63) * EACH, ROW_THREADS * EACH, end, f);
     }
 };
+
+// bf16 elements two at a time, by their bits: those at or above zero are in order as signed numbers, those below it against
+// their order as unsigned ones.
+typedef short s16x2 __attribute__((ext_vector_type(2)));
+typedef unsigned short u16x2 __attribute__((ext_vector_type(2)));
+__device__ __forceinline__ s16x2 signed_pair(uint32_t w) { return __builtin_bit_cast(s16x2, w); }
+__device__ __forceinline__ s16x2 larger(s16x2 a, s16x2 b) { return __builtin_elementwise_max(a, b); }
+
+// A thread's largest logit.
+template <typename T> __device__ __forceinline__ float largest(const Row<T> &row) {
+    float top = -INFINITY;
+    if constexpr (sizeof(T) == 2) {
+        s16x2 most = {-32768, -32768};
+        u16x2 least = {0xffff, 0xffff};
+        row.raw((threadIdx.x & ~63) * EACH, ROW_THREADS * EACH, row.end, [&](const typename Row<T>::Eight &e, int) {
+            const uint32_t w[4] = {e.x[0].x, e.x[0].y, e.x[0].z, e.x[0].w};
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                most = larger(most, signed_pair(w[i]));
+                least = __builtin_elementwise_min(least, __builtin_bit_cast(u16x2, w[i]));
+            }
+        });
+        const short m = max(most.x, most.y);
+        const unsigned short l = min(least.x, least.y);
+        if (m < 0) return fmaxf(__builtin_bit_cast(float, (uint32_t)l << 16), -INFINITY);      // (none at or above zero)
+        top = __builtin_bit_cast(float, (uint32_t)(unsigned short)m << 16);
+        if (top == top) return top;                      // (not a NaN, whose bits are above infinity's)
+        top = -INFINITY;
+    }
+    row.each([&](const float *x, int) {
+#pragma unroll
+        for (int j = 0; j < EACH; ++j) top = fmaxf(top, x[j]);
+    });
+    return top;
+}
 
 struct Shared {
     union {
@@ -165,7 +200,8 @@ struct Shared {
     };
     u64 wave64[WAVES], before64;
     uint32_t wave32[WAVES], before32;
-    float wavef[WAVES];
+    float wavef[WAVES], bound;
+    uint32_t pair_top[PAIRS];
     int at, listed;
 };
 
@@ -230,11 +266,7 @@ template <typename T> __global__ __launch_bounds__(ROW_THREADS, 8) void sample_k
     const int r = blockIdx.x, tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
     const Row<T> row((const T *)a.logits + (int64_t)r * a.row_stride, a.V);
 
-    float mine = -INFINITY;
-    row.each([&](const float *x, int) {
-#pragma unroll
-        for (int j = 0; j < EACH; ++j) mine = fmaxf(mine, x[j]);
-    });
+    const float mine = largest(row);
     float top = mine;
 #pragma unroll
     for (int d = 32; d > 0; d >>= 1) top = fmaxf(top, __shfl_xor(top, d));
@@ -280,14 +312,27 @@ template <typename T> __global__ __launch_bounds__(ROW_THREADS, 8) void sample_k
 
     u64 all = 0;                                         // likelihoods of the whole row, where a top-p alone needs them
     if ((by_count && top_k <= MOST_K) || (!by_count && by_weight)) {
-        // The bound: a value that `want` of the threads' maxima reach, and no other with its low 12 bits clear is larger.
+        // The bound: a value that `want` of the 512 pairs of threads reach, and no other with its low 12 bits clear is larger.
+        // (One wave finds it, eight pairs a lane: a count over the workgroup for each bit took 6 us.)
         const int want = by_count ? top_k : NUCLEUS;
-        const uint32_t mine_key = key_of(mine);
-        uint32_t t = 0;
+        const float pair = fmaxf(mine, __shfl_xor(mine, 1));
+        if ((tid & 1) == 0) s.pair_top[tid / 2] = key_of(pair);
+        __syncthreads();
+        if (wave == 0) {
+            uint32_t k[PAIRS / 64], t = 0;
+#pragma unroll
+            for (int i = 0; i < PAIRS / 64; ++i) k[i] = s.pair_top[i * 64 + lane];
 #pragma unroll 1
-        for (int bit = 31; bit >= 12; --bit)
-            if (__syncthreads_count(mine_key >= (t | 1u << bit)) >= want) t |= 1u << bit;
-        const float bound = t > key_of(-INFINITY) ? of_key(t) : -INFINITY;
+            for (int bit = 31; bit >= 12; --bit) {
+                int n = 0;
+#pragma unroll
+                for (int i = 0; i < PAIRS / 64; ++i) n += __popcll(__ballot(k[i] >= (t | 1u << bit)));
+                if (n >= want) t |= 1u << bit;
+            }
+            if (lane == 0) s.bound = t > key_of(-INFINITY) ? of_key(t) : -INFINITY;
+        }
+        __syncthreads();
+        const float bound = s.bound;
         auto list = [&](const float *x, int v) {
 #pragma unroll
             for (int j = 0; j < EACH; ++j)
@@ -297,7 +342,19 @@ template <typename T> __global__ __launch_bounds__(ROW_THREADS, 8) void sample_k
                 }
         };
         if (by_count) {
-            if (mine >= bound) row.each(list);
+            // (a bf16 row: eight at a time where the bound is above zero, since few reach it)
+            const short bits = sizeof(T) == 2 && bound > 0.0f ? (short)(__builtin_bit_cast(uint32_t, bound) >> 16) : -32768;
+            if (mine >= bound)
+                row.raw((tid & ~63) * EACH, ROW_THREADS * EACH, row.end, [&](const typename Row<T>::Eight &e, int v) {
+                    if constexpr (sizeof(T) == 2) {
+                        const s16x2 m = larger(larger(signed_pair(e.x[0].x), signed_pair(e.x[0].y)),
+                                               larger(signed_pair(e.x[0].z), signed_pair(e.x[0].w)));
+                        if (max(m.x, m.y) < bits) return;
+                    }
+                    float x[EACH];
+                    Row<T>::numbers(e, x);
+                    list(x, v);
+                });
         } else {
             double sum = 0.0;
             row.each([&](const float *x, int v) {
@@ -322,6 +379,7 @@ template <typename T> __global__ __launch_bounds__(ROW_THREADS, 8) void sample_k
             int at = 0;
             if (tid < n) {
                 int t = 0;
+#pragma unroll 4
                 for (; t + 1 < n; t += 2) {
                     const ulonglong2 o = *reinterpret_cast<const ulonglong2 *>(&s.list.key[t]);
                     at += (o.x > key) + (o.y > key);
@@ -349,6 +407,7 @@ template <typename T> __global__ __launch_bounds__(ROW_THREADS, 8) void sample_k
                 const int kept = __syncthreads_count(w > 0);          // a prefix
                 if (w > 0) {
                     u64 sum = 0;                         // kept likelihoods before this token in the vocabulary
+#pragma unroll 4
                     for (int t = 0; t < kept; ++t) sum += s.list.index_at[t] < index ? s.list.weight_at[t] : 0;
                     if (sum <= point && point < sum + w) {
                         answer(a, r, index, scale, to_f32(row.base[row.off + index]), total);
@@ -457,6 +516,10 @@ template <typename T> __global__ __launch_bounds__(ROW_THREADS, 8) void sample_k
 #pragma unroll
         for (int j = 0; j < EACH; ++j) {
             const float f = Scale::scaled(scale.octaves(x[j]));
+            if (cut == 0) {
+                w += exactly(f >= least ? f : 0.0f);
+                continue;
+            }
             w += exactly(f >= least && x[j] > cut_at ? f : 0.0f);
             t += f >= least && x[j] == cut_at;
         }
