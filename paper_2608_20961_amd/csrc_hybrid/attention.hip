@@ -57,6 +57,7 @@ template <typename T_, int HD_, int WR_, int WK_, int KT_, int TURN_> struct Sha
     static constexpr int TURN = TURN_, LO = sizeof(T) == 2 ? TURN : 0;
     static constexpr int TILE = KT * GRAN;               // granules of a tile's keys (and of its values)
     static constexpr int OCCUPANCY = NT >= 512 || (HD <= 128 && sizeof(T) == 2 && 4 * TILE * 16 <= 80 * 1024) ? 2 : 1;
+    static constexpr bool SHARES = RT <= 64 || sizeof(T) == 4;        // whether it takes shared keys (with few rows only: shared_used)
     static constexpr int PAIRS = TILE / 64 / WAVES;      // loads of keys (and of values) that a wave has of a tile
     static constexpr bool REST_LDS = OCCUPANCY == 2 && HD == 256;     // the queries' second parts stay in LDS (registers are short)
     static constexpr bool Q_FIRST = RT * (GRAN + (LO > 0 && !REST_LDS ? 2 * TURN : 0)) > 2 * TILE;    // queries need both tiles' LDS on their way
@@ -419,7 +420,7 @@ template <typename S> __global__ __launch_bounds__(S::NT, S::OCCUPANCY) void att
         const uint32_t page_rows = (1u << log2_page) - 1u;
         const int64_t page_bytes = (int64_t)a.H_kv * ROW << log2_page;
         // the unit: its cached keys [first_key, len) in old_tiles, then the draft's
-        const bool shared = b < 0;
+        const bool shared = S::SHARES && b < 0;
         const int own_b = shared ? longest : b;
         const int len_b = uniform(cached(a, own_b));
         const int first_key = shared ? 0 : min(a.shared, len_b), len = shared ? min(a.shared, len_b) : len_b;
@@ -507,7 +508,7 @@ template <typename S> __global__ __launch_bounds__(S::NT, S::OCCUPANCY) void att
         const bool live = r < (shared ? a.B * w->c.M : w->c.M);
         const int x0 = live ? r : 0, row_b = shared ? x0 / w->c.M : b, rr = shared ? x0 - row_b * w->c.M : x0;
         const int node = rr / w->c.G, head = h * w->c.G + rr - node * w->c.G;
-        const int row_len = cached(a, row_b), limit = min(row_len, len);
+        const int row_len = shared ? cached(a, row_b) : len_b, limit = S::SHARES ? min(row_len, len) : len;
         // Queries go through LDS: a row's granules are read side by side, and the rotation is one short loop (unrolled over a
         // lane's own granules it was a third of the kernel's instructions, each run once and most of them not in the
         // instruction cache).
@@ -669,7 +670,7 @@ template <typename S> __global__ __launch_bounds__(S::NT, S::OCCUPANCY) void att
                 for (int i = 0; i < (S::REST_LDS ? 1 : 2); ++i) read_values(i);
             // What the row does not see: keys past its limit or of invalid pages, nodes that are not its ancestors.
             const uint64_t bad = old ? __ballot(lane < pages_in(t) && now < 0) : 0;
-            if (!old || bad || __any(first + 32 * NB > limit)) {
+            if (!old || bad || (S::SHARES ? __any(first + 32 * NB > limit) : first + 32 * NB > len)) {
 #pragma unroll
                 for (int n = 0; n < NB; ++n) {
                     const int key = first + 32 * n, have = old ? limit - key : node + 1 - key;
@@ -1055,13 +1056,23 @@ int rows_of(int shared, int N, int B, int H_q, int H_kv) {
 
 size_t tree_attention_workspace(int shared, int N, int B, int H_q, int H_kv, int d, bool f32) {
     shared = shared_used(shared, N, B, H_q, H_kv);
-    return choose(rows_of(shared, N, B, H_q, H_kv), d, 0, f32, [&](auto s) { return bytes<decltype(s)>(shared, N, B, H_q, H_kv); });
+    size_t most = 0;                                     // (of the kernels for any rotation)
+    for (const int rot : {0, d})
+        most = std::max(most, choose(rows_of(shared, N, B, H_q, H_kv), d, rot, f32, [&](auto s) {
+            using S = decltype(s);
+            return bytes<S>(S::SHARES ? shared : 0, N, B, H_q, H_kv);
+        }));
+    return most;
 }
 
 hipError_t launch_tree_attention(AttendArgs a, int d, bool f32, void *workspace, hipStream_t stream) {
     a.shared = shared_used(a.shared, a.N, a.B, a.H_q, a.H_kv);
     return choose(rows_of(a.shared, a.N, a.B, a.H_q, a.H_kv), d, a.rot, f32,
-                  [&](auto s) { return run<decltype(s)>(a, workspace, stream); });
+                  [&](auto s) {
+                      using S = decltype(s);
+                      if (!S::SHARES) a.shared = 0;
+                      return run<S>(a, workspace, stream);
+                  });
 }
 
 }  // namespace treewy
