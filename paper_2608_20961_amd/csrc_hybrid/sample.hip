@@ -311,7 +311,11 @@ template <typename T> __global__ __launch_bounds__(ROW_THREADS, 8) void sample_k
     const u64 part = (u64)(fmaxf(top_p, 0.0f) * 0x1p31f);            // top_p of a sum is share(sum, part); 0 where it is off
 
     u64 all = 0;                                         // likelihoods of the whole row, where a top-p alone needs them
-    if ((by_count && top_k <= MOST_K) || (!by_count && by_weight)) {
+    // A top-p alone is worth a list where the pairs' maxima below the bound would not alone be more than it leaves out: they are a
+    // part of what the list leaves out, those at or above it about the list (flat rows: 64 rows of 100003 took 108 us with the
+    // list's pass in vain).
+    bool listed = (by_count && top_k <= MOST_K) || (!by_count && by_weight);
+    if (listed) {
         // The bound: a value that `want` of the 512 pairs of threads reach, and no other with its low 12 bits clear is larger.
         // (One wave finds it, eight pairs a lane: a count over the workgroup for each bit took 6 us.)
         const int want = by_count ? top_k : NUCLEUS;
@@ -333,6 +337,12 @@ template <typename T> __global__ __launch_bounds__(ROW_THREADS, 8) void sample_k
         }
         __syncthreads();
         const float bound = s.bound;
+        if (!by_count) {
+            const u64 w = (tid & 1) == 0 ? scale.of(pair) : 0;
+            u64 before;
+            const u64 above = group_sum(s, pair >= bound ? w : 0, before), below = group_sum(s, pair >= bound ? 0 : w, before);
+            listed = below <= above + below - share(above + below, part);
+        }
         auto list = [&](const float *x, int v) {
 #pragma unroll
             for (int j = 0; j < EACH; ++j)
@@ -341,7 +351,8 @@ template <typename T> __global__ __launch_bounds__(ROW_THREADS, 8) void sample_k
                     if (at < LIST) s.list.key[at] = (u64)key_of(x[j]) << 32 | (uint32_t)~(v + j - row.off);
                 }
         };
-        if (by_count) {
+        if (!listed) {
+        } else if (by_count) {
             // (a bf16 row: eight at a time where the bound is above zero, since few reach it)
             const short bits = sizeof(T) == 2 && bound > 0.0f ? (short)(__builtin_bit_cast(uint32_t, bound) >> 16) : -32768;
             if (mine >= bound)
@@ -371,7 +382,7 @@ template <typename T> __global__ __launch_bounds__(ROW_THREADS, 8) void sample_k
         __syncthreads();
         const int n = s.listed;
         // Rank in the list, and the token in its place.
-        bool done = n <= LIST;
+        bool done = listed && n <= LIST;
         u64 w = 0, total = 0;
         if (done) {
             const u64 key = tid < n ? s.list.key[tid] : 0;
