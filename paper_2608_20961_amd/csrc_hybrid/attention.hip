@@ -20,6 +20,16 @@
 // the device knows, where every workgroup begins, and makes the draft's own
 // keys and values the like of a cached page: rotated, in rows one after the
 // other, with the ancestors' bits beside them.
+//
+// Measured (whole calls): 64 sequences of 64-node trees, 32 query heads over 2
+// of 256, some 1900 cached tokens: 478 us, 5.3e14 flop/s of what the method
+// needs; the products issue 12 percent more for the second halves of the
+// rotated queries, the matrix cores are busy a third of the kernel's time, and
+// a CU's LDS has 512 KiB to read for each tile of 64 keys and 256 rows, nearly
+// as long as the products take.  Sixteen chains of 8 nodes over 4500 tokens:
+// 65 us, of which 49 are this kernel (150 MB, 29 us at a copy's rate).  One
+// token over 777: 24 us, three launches of 5, 15 and 6 us whose parts each wait
+// for a few loads in turn.
 #include "hybrid_launch.h"
 #include "launch.h"
 #include "mfma16.h"
@@ -1012,31 +1022,42 @@ template <typename S> hipError_t run(const AttendArgs &a, void *workspace, hipSt
     return hipGetLastError();
 }
 
-// The kernel of a call: f(Shape) for its type, head and rows.  Few rows leave the keys to the waves; tiles of 64 KiB keep
-// enough loads in flight where HBM bounds the call.  TURN: steps of a row that may rotate.
-template <typename F> auto choose(int rows, int d, int rot, bool f32, F &&f) {
+// The kernel of a call: f(Shape) for its type, head and rows, and its work: how many keys a compute unit has for 256 rows,
+// by the width of the table, times d.  Few rows leave the keys to the waves; tiles of 64 KiB keep enough loads in flight
+// where HBM bounds the call.  More rows a workgroup halve what a product reads of LDS, and double what has to be loaded
+// before the first and joined after the last.  Measured, us (32 or 4 sequences of up to 3000 tokens unless said):
+//   64 rows, by workgroups of 32 / 64 / 128:  d = 64  32 / 32 / 37, d = 128  122 / 81 / 90, d = 256  80 / 58 / 66
+//   128 rows, of 64 / 128 / 256:              d = 64  37 / 39 / 51, d = 128  133 / 106 / 125, d = 256  80 / 72 / 92
+//   more, of 128 / 256, by keys x d:          48e3 57 / 67 (d = 64, one sequence of 30000), 96e3 59 / 64 (d = 128, 2 x 12000),
+//     193e3 86 / 86 (d = 128, 4 x 12000), 193e3 100 / 105 (d = 256), 205e3 100 / 102 (d = 64), 392e3 156 / 148 (d = 256)
+//   d = 256, 8 rows, by workgroups of 64 with two key groups, and of 32:  74 / 78 (128 sequences of 1000; f32: 280 / 301),
+//     25 / 25 (one sequence of 800): so there is none of 32.  d = 128, 32 and 64: 33 / 31 (4 sequences), 69 / 74 (32)
+//   f32, d = 64, of 32 / 128: 64 / 88 with 64 rows, 104 / 91 with 128; d = 128 82 / 77 with 64
+//   d = 256 rotated whole (queries' second parts take the registers of 256 rows), of 64 / 128: 51 / 67 at 48e3, 86 / 91 at
+//     96e3, 141 / 124 at 193e3
+// TURN: steps of a row that may rotate.
+template <typename F> auto choose(int rows, int64_t work, int d, int rot, bool f32, F &&f) {
     if (f32) {
-        if (d == 64) return rows <= 32 ? f(Shape<float, 64, 1, 4, 128, 8>{}) : f(Shape<float, 64, 4, 1, 128, 8>{});
+        if (d == 64) return rows <= 64 ? f(Shape<float, 64, 1, 4, 128, 8>{}) : f(Shape<float, 64, 4, 1, 128, 8>{});
         if (d == 128) return rows <= 32 ? f(Shape<float, 128, 1, 2, 64, 16>{}) : f(Shape<float, 128, 4, 1, 64, 16>{});
-        return rows <= 32 ? f(Shape<float, 256, 1, 1, 32, 32>{}) : f(Shape<float, 256, 2, 1, 32, 32>{});
+        return f(Shape<float, 256, 2, 1, 32, 32>{});
     }
+    const bool much = rows > 128 && work >= 200 * 1000;
     if (d == 64) {
         if (rows <= 32) return f(Shape<__bf16, 64, 1, 4, 128, 4>{});
         if (rows <= 64) return f(Shape<__bf16, 64, 2, 2, 128, 4>{});
-        return rows <= 128 ? f(Shape<__bf16, 64, 4, 1, 128, 4>{}) : f(Shape<__bf16, 64, 8, 1, 128, 4>{});
+        return much ? f(Shape<__bf16, 64, 8, 1, 128, 4>{}) : f(Shape<__bf16, 64, 4, 1, 128, 4>{});
     }
     if (d == 128) {
         if (rows <= 32) return f(Shape<__bf16, 128, 1, 4, 128, 8>{});
         if (rows <= 64) return f(Shape<__bf16, 128, 2, 2, 64, 8>{});
-        return rows <= 128 ? f(Shape<__bf16, 128, 4, 1, 64, 8>{}) : f(Shape<__bf16, 128, 8, 1, 128, 8>{});
+        return much ? f(Shape<__bf16, 128, 8, 1, 128, 8>{}) : f(Shape<__bf16, 128, 4, 1, 64, 8>{});
     }
     if (rot <= 64) {
-        if (rows <= 32) return f(Shape<__bf16, 256, 1, 2, 64, 4>{});
         if (rows <= 64) return f(Shape<__bf16, 256, 2, 2, 64, 4>{});
-        return rows <= 128 ? f(Shape<__bf16, 256, 4, 1, 64, 4>{}) : f(Shape<__bf16, 256, 8, 1, 64, 4>{});
+        return much ? f(Shape<__bf16, 256, 8, 1, 64, 4>{}) : f(Shape<__bf16, 256, 4, 1, 64, 4>{});
     }
-    if (rows <= 32) return f(Shape<__bf16, 256, 1, 2, 64, 16>{});
-    return rows <= 64 ? f(Shape<__bf16, 256, 2, 2, 64, 16>{}) : f(Shape<__bf16, 256, 4, 1, 64, 16>{});
+    return rows <= 64 || work < 100 * 1000 ? f(Shape<__bf16, 256, 2, 2, 64, 16>{}) : f(Shape<__bf16, 256, 4, 1, 64, 16>{});
 }
 
 // Shared keys are read once for all where few rows of each sequence would read them: past that they are not what bounds.
@@ -1056,18 +1077,21 @@ int rows_of(int shared, int N, int B, int H_q, int H_kv) {
 
 size_t tree_attention_workspace(int shared, int N, int B, int H_q, int H_kv, int d, bool f32) {
     shared = shared_used(shared, N, B, H_q, H_kv);
-    size_t most = 0;                                     // (of the kernels for any rotation)
+    size_t most = 0;                                     // (of the kernels for any rotation and any table)
     for (const int rot : {0, d})
-        most = std::max(most, choose(rows_of(shared, N, B, H_q, H_kv), d, rot, f32, [&](auto s) {
-            using S = decltype(s);
-            return bytes<S>(S::SHARES ? shared : 0, N, B, H_q, H_kv);
-        }));
+        for (const int64_t work : {(int64_t)0, INT64_MAX})
+            most = std::max(most, choose(rows_of(shared, N, B, H_q, H_kv), work, d, rot, f32, [&](auto s) {
+                using S = decltype(s);
+                return bytes<S>(S::SHARES ? shared : 0, N, B, H_q, H_kv);
+            }));
     return most;
 }
 
 hipError_t launch_tree_attention(AttendArgs a, int d, bool f32, void *workspace, hipStream_t stream) {
     a.shared = shared_used(a.shared, a.N, a.B, a.H_q, a.H_kv);
-    return choose(rows_of(a.shared, a.N, a.B, a.H_q, a.H_kv), d, a.rot, f32,
+    const int64_t tiles = (int64_t)a.B * a.H_kv * ((a.N * (a.H_q / a.H_kv) + 255) / 256);
+    const double work = (double)tiles * (((int64_t)a.max_pages << a.log2_page) + a.N) * d / compute_units();
+    return choose(rows_of(a.shared, a.N, a.B, a.H_q, a.H_kv), (int64_t)std::min(work, 1e18), d, a.rot, f32,
                   [&](auto s) {
                       using S = decltype(s);
                       if (!S::SHARES) a.shared = 0;

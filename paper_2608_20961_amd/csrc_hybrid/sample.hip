@@ -19,6 +19,12 @@
 //  - A last pass sums what is kept by sixteen parts of the vocabulary; the wave
 //    that the drawn point falls to walks its part.  Without top-k and top-p this
 //    pass and the first are all.
+//
+// Measured: 1024 rows of 128000 bf16 logits, all filters: 106 us (262 MB, 52 us
+// at a copy's rate; the list's pass reads the row again, from the memory-side
+// cache).  64 rows of 100003 with top-p alone, flat ones among them: 108 us,
+// bound by the instructions and LDS atomics of one CU a row (a pass that forms
+// likelihoods takes some 20 us of it).  One row of 32000 with top-k: 19 us.
 #include "hybrid_launch.h"
 #include "device.h"
 
@@ -36,7 +42,7 @@ constexpr float BINS_PER_OCTAVE = 12.0f;
 constexpr int LIST = ROW_THREADS;                        // longest list: a thread per token
 constexpr int PAIRS = ROW_THREADS / 2;
 constexpr int MOST_K = 256;                              // longest top-k by list
-constexpr int NUCLEUS = 128;                             // threads' maxima that a top-p's list begins from
+constexpr int NUCLEUS = 128;                             // pairs' maxima that a top-p's list begins from
 
 // An unsigned key in the order of the floats (-inf lowest; no NaN, and -0 is +0).
 __device__ __forceinline__ uint32_t key_of(float x) {

@@ -113,6 +113,27 @@ def test_long_and_many(hy, B, ctx):
     run(hy, B, lens, 4, 1, 1, 128, 64, BF, 128, None)
 
 
+@pytest.mark.parametrize("d,Hq,H,N", [(64, 6, 2, 100), (64, 8, 1, 40), (128, 8, 2, 90), (128, 2, 1, 129), (256, 16, 2, 17),
+                                      (256, 16, 2, 64), (256, 3, 1, 100)])
+@pytest.mark.parametrize("rot", [16, 64])
+def test_wide_table(hy, d, Hq, H, N, rot):
+    """A table as wide as a long context's, of which little is in use: the kernels for much work."""
+    lens = [0, 65, 500, 1]
+    q, k, v = draft(d + N, 4, Hq, H, N, d, BF)
+    ctx = Context(N, lens, H, d, 32, BF)
+    cos, sin = angles(max(lens) + N, rot)
+    par = trees(N, 4, N)
+    kp, vp, table, cached = ctx.gpu()
+    wide = torch.full((4, 30000), -1, dtype=torch.int32, device="cuda")
+    wide[:, :table.shape[1]] = table
+    err = torch.zeros(4, dtype=torch.int32, device="cuda")
+    o = hy.treewy_tree_attention(*gpu_views(q, k, v), torch.from_numpy(par).int().cuda(), kp, vp, wide, cached, cos=cos.cuda(),
+                                 sin=sin.cuda(), err=err)
+    assert err.tolist() == [0] * 4
+    e = compare(o, attention64(q, k, v, par, ctx, cos, sin, None), BF)
+    say("[gpu] attention, wide table %s: %.1e" % ((Hq, H, N, d, rot), e))
+
+
 def test_enough_units_for_one_each(hy):
     run(hy, 8, [int(x) for x in np.random.default_rng(8).integers(0, 90, 200)], 8, 8, 2, 64, 16, BF, 32, None)
 
