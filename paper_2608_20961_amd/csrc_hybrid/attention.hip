@@ -16,18 +16,20 @@
 // by sequence), of which every workgroup takes an equal, consecutive part,
 // however ragged the lengths.  A row tile ("unit") that one workgroup has
 // whole is written at once; the parts of others go to the workspace and are
-// joined by a last launch.  A first launch finds, from the lengths that only
-// the device knows, where every workgroup begins, and makes the draft's own
+// joined by a last launch.  Where there are as many units as workgroups or
+// more they are left whole, longest first, unless one is so long that the rest
+// would wait for it.  A first launch finds, from the lengths that only the
+// device knows, what every workgroup takes, and makes the draft's own
 // keys and values the like of a cached page: rotated, in rows one after the
 // other, with the ancestors' bits beside them.
 //
 // Measured (whole calls): 64 sequences of 64-node trees, 32 query heads over 2
-// of 256, some 1900 cached tokens: 478 us, 5.3e14 flop/s of what the method
-// needs; the products issue 12 percent more for the second halves of the
-// rotated queries, the matrix cores are busy a third of the kernel's time, and
+// of 256, some 1900 cached tokens: 385 to 410 us, 6.4e14 flop/s of what the
+// method needs; the products issue 12 percent more for the second halves of the
+// rotated queries, the matrix cores are busy two fifths of the kernel's time, and
 // a CU's LDS has 512 KiB to read for each tile of 64 keys and 256 rows, nearly
 // as long as the products take.  Sixteen chains of 8 nodes over 4500 tokens:
-// 65 us, of which 49 are this kernel (150 MB, 29 us at a copy's rate).  One
+// 62 us, of which 48 are this kernel (150 MB, 29 us at a copy's rate).  One
 // token over 777: 24 us, three launches of 5, 15 and 6 us whose parts each wait
 // for a few loads in turn.
 #include "hybrid_launch.h"
@@ -95,6 +97,8 @@ struct Cut {
     int shared_tiles;                                    // key tiles of the shared keys
     int draft_tiles;                                     // summed over a (sequence, head)'s row tiles
     int groups;                                          // workgroups that share the list; 0: one per unit
+    int records;                                         // workgroups in all
+    bool whole;                                          // whether units may be left whole: records are as many
     int64_t slots;
 };
 
@@ -107,12 +111,13 @@ __host__ __device__ inline int draft_tiles_of(int unit, int RT, int KT, int G, i
 struct Start {
     int b, h, rt, t0, tiles, group, longest, pad;        // b = -1: shared keys, rt among a head's shared units; group: its place
 };                                                       // in the list; longest: a sequence with the most cached tokens
+constexpr int MOST_SORTED = 512;                         // sequences
 
 // What the first launch leaves in the workspace (pointers into it).
 struct Prepared {
     int64_t *first;                                      // [B + 1] first tile of each sequence
     Start *start;                                        // [workgroups of the kernel]
-    int *info;                                           // groups that have tiles
+    int *info;                                           // groups that have tiles (0: units were left whole)
     int *depth;                                          // [B][N] ancestors
     uint32_t *sees;                                      // [B][N][words] ancestors and self, a bit each (null: a chain)
     uint8_t *odd;                                        // [B][H_kv][N] whether a node's values hold an infinity or NaN
@@ -179,6 +184,51 @@ template <typename T> __device__ __forceinline__ uint4 finite(uint4 x) {
     return Granule<T>::narrow(f);
 }
 
+// Every unit by one workgroup, the longest first, if that is not slower than equal parts.  Its time in tiles: pairs of a long and
+// a short one where they are at most two a workgroup, else the rounds one by one, or the mean and half of one of the last.  A
+// part costs its workgroup and the join some 3 RT / KT tiles' time (256 rows of 256, 256 units of some 40 tiles at most: 259 us
+// whole and 278 in parts; of some 95: 621 and 560; 512 of some 39: 409 and 475).  Whether it has been done.
+__device__ bool leave_whole(const Work &w, int RT, int KT, int64_t total) {
+    __shared__ int tiles[MOST_SORTED], sorted[MOST_SORTED], who[MOST_SORTED], pairs_most;
+    const AttendArgs &a = w.a;
+    const int tid = threadIdx.x, m = w.c.groups, all = w.c.records, pairs = a.B * a.H_kv, per = w.c.units, each = a.H_kv * per;
+    const int draft = draft_tiles_of(per - 1, RT, KT, w.c.G, a.N);
+    for (int b = tid; b < a.B; b += THREADS) tiles[b] = own_tiles(a, KT, cached(a, b)) + draft;
+    if (tid == 0) pairs_most = 0;
+    __syncthreads();
+    for (int b = tid; b < a.B; b += THREADS) {
+        int rank = 0;
+        for (int i = 0; i < a.B; ++i) rank += tiles[i] > tiles[b] || (tiles[i] == tiles[b] && i < b);
+        sorted[rank] = tiles[b];
+        who[rank] = b;
+    }
+    __syncthreads();
+    for (int i = tid; i < m; i += THREADS)
+        if (i < all) atomicMax(&pairs_most, sorted[i / each] + (2 * m - 1 - i < all ? sorted[(2 * m - 1 - i) / each] : 0));
+    __syncthreads();
+    int64_t most = pairs_most;
+    if (all > 2 * m) {
+        most = 0;
+        for (int i = 0; i < all; i += m) most += sorted[i / each];
+        most = min(most, total / m + sorted[a.B - 1] / 2);
+    }
+    if (most > total / m + 3 * RT / KT) return false;
+    // (the row tiles of a head's keys on one XCD)
+    const int even = pairs / 8 * 8;
+    for (int p = tid; p < pairs; p += THREADS) {
+        Start s{};
+        s.b = who[p / a.H_kv];
+        s.h = p % a.H_kv;
+        const int old = tiles[s.b] - draft;
+        for (s.rt = 0; s.rt < per; ++s.rt) {
+            s.tiles = old + draft_tiles_of(s.rt, RT, KT, w.c.G, a.N);
+            w.p.start[p < even ? (p / 8 * per + s.rt) * 8 + p % 8 : p * per + s.rt] = s;
+        }
+    }
+    if (tid == 0) w.p.info[0] = 0;
+    return true;
+}
+
 // The list: first tiles, and where every group begins.  One workgroup.
 __device__ void make_list(const Work &w, int RT, int KT) {
     constexpr int WAVES = THREADS / 64;
@@ -218,6 +268,7 @@ __device__ void make_list(const Work &w, int RT, int KT) {
         next += tiles_of(b);
     }
     if (tid == 0) w.p.first[a.B] = total;
+    if (w.c.whole && leave_whole(w, RT, KT, total)) return;
     const int groups = (int)min((int64_t)w.c.groups, total);
     if (tid == 0) w.p.info[0] = groups;
     __threadfence_block();
@@ -225,7 +276,7 @@ __device__ void make_list(const Work &w, int RT, int KT) {
     // Consecutive parts on one XCD (workgroups go to the eight in turn): row tiles that read the same keys meet in its L2.  Where
     // there are fewer tiles than workgroups they have one each, on all XCDs.
     const int per_xcd = w.c.groups / 8;
-    for (int i = tid; i < w.c.groups; i += THREADS) {
+    for (int i = tid; i < w.c.records; i += THREADS) {
         const int g = groups < w.c.groups || i >= per_xcd * 8 ? i : (i & 7) * per_xcd + (i >> 3);
         Start s{};
         if (g >= groups) {
@@ -873,13 +924,15 @@ template <typename S, bool MANY> __global__ __launch_bounds__(256) void join_ker
     using T = typename S::T;
     __shared__ float sums[MANY ? 1 : 4][17][64], tops[4][64];
     const AttendArgs &a = w.a;
+    const int groups = w.p.info[0];
+    if (groups == 0) return;                             // all written already
     const int lane = threadIdx.x & 63, wave = uniform(threadIdx.x >> 6), hg = lane >> 5;
     const int at_unit = MANY ? blockIdx.x : blockIdx.x / DT, wr = at_unit % S::WR, unit = at_unit / S::WR;
     const int b = unit / (a.H_kv * w.c.units), n = unit - b * a.H_kv * w.c.units, h = n / w.c.units, rt = n - h * w.c.units;
     const int r = rt * RT + wr * 32 + (lane & 31);
     if (rt * RT + wr * 32 >= w.c.M) return;
     const int64_t total = w.p.first[a.B], before = w.p.first[b];
-    const int groups = w.p.info[0], old = own_tiles(a, KT, cached(a, b));
+    const int old = own_tiles(a, KT, cached(a, b));
     int64_t begin = before + (int64_t)h * (w.c.units * old + w.c.draft_tiles);
     for (int i = 0; i < rt; ++i) begin += old + draft_tiles_of(i, RT, KT, w.c.G, a.N);
     const int64_t end = begin + old + draft_tiles_of(rt, RT, KT, w.c.G, a.N);
@@ -966,8 +1019,10 @@ template <typename S> Cut cut(int shared, int N, int B, int H_q, int H_kv) {
         c.shared_tiles = (shared + S::KT - 1) / S::KT;
     }
     const int resident = compute_units() * (4 * S::TILE * 16 > 80 * 1024 ? 1 : 2);
-    if (shared == 0 && all >= 3 * (int64_t)resident) return c;      // enough units to even themselves out
+    c.whole = shared == 0 && all >= resident && all < 8 * (int64_t)resident && B <= MOST_SORTED;
+    if (shared == 0 && all >= 3 * (int64_t)resident && !c.whole) return c;    // enough units to even themselves out
     c.groups = resident;
+    c.records = c.whole ? (int)all : resident;
     c.slots = 2 * (int64_t)resident + (shared > 0 ? (int64_t)H_kv * c.shared_units + all : 0);
     return c;
 }
@@ -985,7 +1040,7 @@ template <typename S> size_t lay_out(Work &w, void *workspace) {
     const size_t rows = (size_t)a.B * a.H_kv * a.N;
     take(w.p.first, a.B + 1);
     take(w.p.info, 1);
-    take(w.p.start, w.c.groups);
+    take(w.p.start, w.c.records);
     take(w.p.odd, rows);
     take(w.p.depth, (size_t)a.B * a.N);
     take(w.p.sees, (size_t)a.B * a.N * w.words);
@@ -1013,7 +1068,7 @@ template <typename S> hipError_t run(const AttendArgs &a, void *workspace, hipSt
     w.prep_blocks = (int)((pairs + 4 * THREADS - 1) / (4 * THREADS));
     hipLaunchKernelGGL((prepare_kernel<typename S::T, S::HD>), dim3((unsigned)(a.B * w.prep_blocks + 1)), dim3(THREADS), 0, stream, w,
                        S::RT, S::KT);
-    hipLaunchKernelGGL((attend_kernel<S>), dim3((unsigned)(w.c.groups ? w.c.groups : units)), dim3(S::NT), 0, stream, w);
+    hipLaunchKernelGGL((attend_kernel<S>), dim3((unsigned)(w.c.groups ? w.c.records : units)), dim3(S::NT), 0, stream, w);
     // (the first form from as many workgroups as fill the device; 16 x 8-node chains, 16 parts each, took 7.6 us by the second)
     if (w.c.groups && units * S::WR >= 2 * compute_units())
         hipLaunchKernelGGL((join_kernel<S, true>), dim3((unsigned)(units * S::WR)), dim3(256), 0, stream, w);

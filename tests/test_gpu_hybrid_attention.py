@@ -138,6 +138,17 @@ def test_enough_units_for_one_each(hy):
     run(hy, 8, [int(x) for x in np.random.default_rng(8).integers(0, 90, 200)], 8, 8, 2, 64, 16, BF, 32, None)
 
 
+@pytest.mark.parametrize("B,H,N,d", [(64, 4, 1, 256), (87, 3, 3, 256), (64, 8, 1, 64), (131, 4, 2, 128), (500, 2, 1, 64),
+                                     (40, 8, 70, 128), (520, 1, 1, 64)])
+@pytest.mark.parametrize("kind", ["equal", "ragged", "one long", "none"])
+def test_units_whole_or_in_parts(hy, B, H, N, d, kind):
+    """About as many (sequence, head)s as workgroups: whole, or cut where one is longer than the rest together."""
+    lens = {"equal": [64] * B, "ragged": [int(x) for x in np.random.default_rng(B).integers(0, 400, B)],
+            "one long": [3] * (B // 2) + [9000] + [5] * (B - B // 2 - 1), "none": [0] * B}[kind]
+    o = run(hy, B + d, lens, H, H, N, d, 16, BF, 32, trees(B, B, N))
+    assert torch.equal(o, run(hy, B + d, lens, H, H, N, d, 16, BF, 32, trees(B, B, N)))
+
+
 @pytest.mark.parametrize("scale", [-0.1, 0.0, 1.7])
 @pytest.mark.parametrize("dtype", [BF, F32])
 def test_scales(hy, scale, dtype):
