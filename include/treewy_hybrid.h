@@ -96,8 +96,9 @@ treewy_status treewy_cache_append(const void *k, treewy_strides k_strides, const
  *   err      [B] int32 or NULL             BAD_PARENT (that parent counts as -1), BAD_PAGE, CACHE_FULL (a length outside
  *                                          the table counts as the nearest inside; past the rotation table its last row)
  * 1 <= N <= 256, d is 64, 128 or 256, H_q a multiple of H_kv.  Scores, softmax and sums are fp32; bf16 calls round the rotated
- * q and k, the likelihoods that multiply v, and o.  Neither rows past len[b] in a page nor pages past it are used, whatever
- * they hold.  Every call repeats itself bit for bit.
+ * k, the likelihoods that multiply v, and o; the rotated q is kept to 16 bits.  Neither rows past len[b] in a page nor pages
+ * past it are used, whatever they hold.  Every call repeats itself bit for bit; the order of sums follows from the sizes, the
+ * lengths and the table's width, so that a sequence in another batch or under a wider table may differ in its last bits.
  */
 treewy_status treewy_tree_attention(const void *q, treewy_strides q_strides, const void *k, treewy_strides k_strides,
                                     const void *v, treewy_strides v_strides, const int32_t *parent, const treewy_cache *cache,

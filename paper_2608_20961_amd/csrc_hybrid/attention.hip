@@ -29,7 +29,7 @@
 // rotated queries, the matrix cores are busy two fifths of the kernel's time, and
 // a CU's LDS has 512 KiB to read for each tile of 64 keys and 256 rows, nearly
 // as long as the products take.  Sixteen chains of 8 nodes over 4500 tokens:
-// 62 us, of which 48 are this kernel (150 MB, 29 us at a copy's rate).  One
+// 60 to 66 us, of which 48 are this kernel (150 MB, 29 us at a copy's rate).  One
 // token over 777: 24 us, three launches of 5, 15 and 6 us whose parts each wait
 // for a few loads in turn.
 #include "hybrid_launch.h"
@@ -206,13 +206,14 @@ __device__ bool leave_whole(const Work &w, int RT, int KT, int64_t total) {
     for (int i = tid; i < m; i += THREADS)
         if (i < all) atomicMax(&pairs_most, sorted[i / each] + (2 * m - 1 - i < all ? sorted[(2 * m - 1 - i) / each] : 0));
     __syncthreads();
+    const int64_t mean = total / m;
     int64_t most = pairs_most;
     if (all > 2 * m) {
         most = 0;
         for (int i = 0; i < all; i += m) most += sorted[i / each];
-        most = min(most, total / m + sorted[a.B - 1] / 2);
+        most = min(most, mean + sorted[a.B - 1] / 2);
     }
-    if (most > total / m + 3 * RT / KT) return false;
+    if (most > mean + 3 * RT / KT) return false;
     // (the row tiles of a head's keys on one XCD)
     const int even = pairs / 8 * 8;
     for (int p = tid; p < pairs; p += THREADS) {
