@@ -1116,10 +1116,19 @@ template <typename F> auto choose(int rows, int64_t work, int d, int rot, bool f
     return rows <= 64 || work < 100 * 1000 ? f(Shape<__bf16, 256, 2, 2, 64, 16>{}) : f(Shape<__bf16, 256, 4, 1, 64, 16>{});
 }
 
-// Shared keys are read once for all where few rows of each sequence would read them: past that they are not what bounds.
-// Whole tiles only; what is left of the last belongs to each sequence.
-int shared_used(int shared, int N, int B, int H_q, int H_kv) {
-    return B > 1 && N * (H_q / H_kv) <= 64 && N <= 16 ? shared / 128 * 128 : 0;
+// Shared keys are read once for all where few rows of each sequence would read them, and where what is not read again is worth
+// the parts that every sequence then has to join: enough in all, and enough for a sequence's rows.  Whole tiles only; what is
+// left of the last belongs to each sequence.
+// Measured, us, shared / not, by rows of a sequence and MB not read (8 heads of 128 or 2 of 256, 2 to 64 sequences):
+//   4 rows 15 MB 29 / 30, 66 MB 56 / 73, 2.1 GB 82 / 309    8 rows (d = 256) 17 MB 47 / 45, 33 MB 58 / 51, 117 MB 49 / 55
+//   16 rows 15 MB 31 / 30, 66 MB 64 / 74, 2.1 GB 137 / 309  32 rows 33 MB 41 / 37, 117 MB (d = 256) 52 / 56, 2.1 GB 218 / 310
+//   64 rows 66 MB 81 / 56, 2.1 GB 395 / 328, 1.1 GB (d = 256) 266 / 194
+// 256 keys for 64 sequences with 16 heads of 64: 16 rows 74 / 65, 32 rows 84 / 67; 2048 keys 91 / 117 and 116 / 119.  fp32 heads of
+// 64, whose workgroups have 32 rows: 16 rows 156 / 189 and 356 / 502, 32 rows 225 / 190 and 637 / 503.
+int shared_used(int shared, int N, int B, int H_q, int H_kv, int d, bool f32) {
+    const int64_t rows = (int64_t)N * (H_q / H_kv), whole = shared / 128 * 128;
+    const double saved = 2.0 * (B - 1) * H_kv * d * (f32 ? 4 : 2) * whole;
+    return rows <= (f32 && d == 64 ? 16 : 32) && saved >= 2e6 * std::max(rows, (int64_t)20) && whole * d >= 2048 * rows ? (int)whole : 0;
 }
 
 // Rows by which a call's kernel is chosen: those of a sequence, or where keys are shared at most 64 of the batch (the tiles of each
@@ -1132,7 +1141,7 @@ int rows_of(int shared, int N, int B, int H_q, int H_kv) {
 }  // namespace
 
 size_t tree_attention_workspace(int shared, int N, int B, int H_q, int H_kv, int d, bool f32) {
-    shared = shared_used(shared, N, B, H_q, H_kv);
+    shared = shared_used(shared, N, B, H_q, H_kv, d, f32);
     size_t most = 0;                                     // (of the kernels for any rotation and any table)
     for (const int rot : {0, d})
         for (const int64_t work : {(int64_t)0, INT64_MAX})
@@ -1144,7 +1153,7 @@ size_t tree_attention_workspace(int shared, int N, int B, int H_q, int H_kv, int
 }
 
 hipError_t launch_tree_attention(AttendArgs a, int d, bool f32, void *workspace, hipStream_t stream) {
-    a.shared = shared_used(a.shared, a.N, a.B, a.H_q, a.H_kv);
+    a.shared = shared_used(a.shared, a.N, a.B, a.H_q, a.H_kv, d, f32);
     const int64_t tiles = (int64_t)a.B * a.H_kv * ((a.N * (a.H_q / a.H_kv) + 255) / 256);
     const double work = (double)tiles * (((int64_t)a.max_pages << a.log2_page) + a.N) * d / compute_units();
     return choose(rows_of(a.shared, a.N, a.B, a.H_q, a.H_kv), (int64_t)std::min(work, 1e18), d, a.rot, f32,

@@ -100,6 +100,40 @@ def test_shared_prefix(hy, dtype, d, Hq, H, N, B):
     run(hy, B + d, lens, Hq, H, N, d, 16, dtype, 32, None, shared=shared, told=0)
 
 
+@pytest.mark.parametrize("dtype", [BF, F32])
+@pytest.mark.parametrize("d,Hq,H,N,B", [(128, 8, 8, 1, 20), (128, 32, 8, 8, 20), (256, 32, 4, 2, 24), (64, 16, 16, 3, 30),
+                                          (64, 16, 16, 32, 20)])
+def test_shared_prefix_of_many(hy, dtype, d, Hq, H, N, B):
+    """Enough shared keys that reading them once pays; sequences that end inside them and with them."""
+    rng = np.random.default_rng(B)
+    shared = 1100
+    lens = [int(x) for x in rng.integers(shared, shared + 200, B)]
+    lens[0], lens[1], lens[2] = 40, shared, 1024
+    for told in (shared, 1024, 5000):
+        if told == 5000:
+            lens = [shared - 50] * B
+        run(hy, B + d, lens, Hq, H, N, d, 32, dtype, 32, trees(B, B, N), shared=shared, told=min(told, max(lens)))
+
+
+@pytest.mark.parametrize("dtype", [BF, F32])
+def test_bad_page_among_the_shared(hy, dtype):
+    """Its keys are left out for every sequence, which are all told; as without shared_len."""
+    B, H, d, shared = 20, 8, 128, 1024
+    lens = [shared + 30 * b for b in range(B)]
+    lens[3] = 60
+    q, k, v = draft(5, B, H, H, 1, d, dtype)
+    ctx = Context(5, lens, H, d, 32, dtype, shared=shared)
+    kp, vp, table, cached = ctx.gpu()
+    table[:, 7] = kp.shape[0] + 9
+    table[3, 7] = 0
+    out = []
+    for told in (0, shared):
+        err = torch.zeros(B, dtype=torch.int32, device="cuda")
+        out.append(hy.treewy_tree_attention(*gpu_views(q, k, v), None, kp, vp, table, cached, shared_len=told, err=err))
+        assert err.tolist() == [0 if b == 3 else 4 for b in range(B)]
+    compare(out[1], out[0].double().cpu(), dtype)
+
+
 def test_shared_longer_than_any(hy):
     run(hy, 3, [50, 50, 0], 4, 1, 1, 128, 16, BF, 0, None, shared=50, told=5000)
 
