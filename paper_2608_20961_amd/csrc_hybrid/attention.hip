@@ -1020,6 +1020,7 @@ template <typename S> Cut cut(int shared, int N, int B, int H_q, int H_kv) {
         c.shared_tiles = (shared + S::KT - 1) / S::KT;
     }
     const int resident = compute_units() * (4 * S::TILE * 16 > 80 * 1024 ? 1 : 2);
+    // (whole units have to be sorted by one workgroup, and a record each; many more are even enough in the order they come)
     c.whole = shared == 0 && all >= resident && all < 8 * (int64_t)resident && B <= MOST_SORTED;
     if (shared == 0 && all >= 3 * (int64_t)resident && !c.whole) return c;    // enough units to even themselves out
     c.groups = resident;
@@ -1070,7 +1071,8 @@ template <typename S> hipError_t run(const AttendArgs &a, void *workspace, hipSt
     hipLaunchKernelGGL((prepare_kernel<typename S::T, S::HD>), dim3((unsigned)(a.B * w.prep_blocks + 1)), dim3(THREADS), 0, stream, w,
                        S::RT, S::KT);
     hipLaunchKernelGGL((attend_kernel<S>), dim3((unsigned)(w.c.groups ? w.c.records : units)), dim3(S::NT), 0, stream, w);
-    // (the first form from as many workgroups as fill the device; 16 x 8-node chains, 16 parts each, took 7.6 us by the second)
+    // (the first form from as many workgroups as fill the device: with fewer, the whole call 61 us by it and 35 by the second for
+    // 4 sequences and 32 rows of 256; with more, 179 by the second and 174 by the first for 32 and 256 rows of 128)
     if (w.c.groups && units * S::WR >= 2 * compute_units())
         hipLaunchKernelGGL((join_kernel<S, true>), dim3((unsigned)(units * S::WR)), dim3(256), 0, stream, w);
     else if (w.c.groups)
